@@ -306,6 +306,107 @@ int moba_decode_forward_ws(const moba_shape* shape, int32_t q_len, const void* Q
                            float* lse, int32_t* topk_idx, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * The other layers of the paper's hybrid models (sliding-window attention with rotary positions in
+ * every other layer, dense attention in place of MoBA): causal attention to the last `window` keys, its
+ * backward, and rotary positions.
+ */
+typedef struct moba_window_shape {
+    int32_t batch, heads;
+    int32_t kv_heads;      /* grouped-query / multi-query attention, as in moba_shape; 0 = heads   */
+    int32_t q_len, kv_len; /* the queries are the LAST q_len of kv_len positions (training: equal) */
+    int32_t kv_rows;       /* rows that a slice of K and V (and dK, dV) takes in memory, e.g. a cache
+                            * with room to grow; 0 = kv_len.  Rows from kv_len on are neither read
+                            * nor written.                                                       */
+    int32_t head_dim;      /* 64 or 128                                                          */
+    int32_t window;        /* keys that a query attends, itself included; 0 = all up to itself   */
+    int32_t dtype;         /* moba_dtype                                                         */
+    float   softmax_scale; /* <= 0 selects 1/sqrt(head_dim)                                      */
+} moba_window_shape;
+
+/*
+ * The query at position t = kv_len - q_len + r attends the keys u with
+ *   max(0, t - window + 1, first_key[b][r]) <= u <= t,
+ *   O = sum_u p_u v_u, p = softmax(scale * q . k_u), lse = log sum_u exp(scale * q . k_u).
+ * A row whose first_key lies behind t attends nothing: O = 0, lse = -inf, zero gradients, whatever its
+ * Q and dO hold.  A row's results do not depend on what stands in keys, values and queries outside its
+ * pairs, infinities and NaN included (calls that meet those take longer).
+ *   Q          in   [b,heads,q_len,d] dtype
+ *   K, V       in   [b,kv,kv_rows,d] dtype
+ *   first_key  in   [b,q_len] int32, or NULL = 0: first key of the sequence that the row belongs to, for
+ *                   packed batches (moba_varlen_first_key) and padded ones; any values
+ *   O          out  [b,heads,q_len,d] dtype;   lse out [b,heads,q_len] fp32
+ *   ws              at least the bytes that moba_window_workspace names (may be NULL where that is 0), of
+ *                   any content, used by one call at a time
+ * Tensors of dtype and ws start on 16-byte boundaries, lse and first_key on 4-byte ones (else MOBA_EINVAL).  kv_len <= kv_rows <= 2^24,
+ * q_len <= kv_len, batch * heads <= 65535; otherwise MOBA_EINVAL or, for the two limits,
+ * MOBA_EUNSUPPORTED.  Results are the same in every run.
+ */
+int moba_window_workspace(const moba_window_shape* shape, size_t* fwd_ws, size_t* bwd_ws);
+int moba_window_forward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,
+                        const int32_t* first_key, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward, which recomputes the probabilities: D = rowsum(dO o O), P = exp(scale * Q K^T - lse),
+ * dV = P^T dO, dS = P o (dO V^T - D), dQ = scale * dS K, dK = scale * dS^T Q.
+ *   Q, O, dO   in   [b,heads,q_len,d] dtype;   lse in [b,heads,q_len] fp32 (from moba_window_forward)
+ *   dQ         out  [b,heads,q_len,d] dtype
+ *   dK, dV     out  [b,kv,kv_rows,d] dtype, rows below kv_len, summed over the query heads that share the
+ *                   head; keys that no row attends get zeros
+ * No output may overlap an input or another output.
+ */
+int moba_window_backward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,
+                         const void* O, const float* lse, const void* dO, const int32_t* first_key,
+                         void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * first_key of a packed batch: offsets[i] of the sequence that row t belongs to, for every row below
+ * offsets[num_seqs] (device arrays; seq_offsets for the packed layout, pad_offsets for the padded one,
+ * whose padding rows then attend like rows of the sequence before them).
+ */
+int moba_varlen_first_key(int32_t num_seqs, const int32_t* offsets, int32_t tokens, int32_t* first_key, void* stream);
+
+/*
+ * Rotary positions.  The first rot_dim channels of a row form rot_dim / 2 pairs; pair i of the row at
+ * position p is turned by the angle p * f_i and scaled by the amplitude a,
+ *   (x, y) -> a (x cos - y sin, y cos + x sin),
+ *   f_i = g_i (keep_i + (1 - keep_i) / scale_factor),   g_i = theta^(-2 i / rot_dim),
+ * keep_i = 0 where orig_len is 0 (positions divided by scale_factor), else the share of its own speed
+ * that a pair keeps in a context stretched beyond orig_len positions, by its turns within those,
+ *   keep_i = clamp((orig_len g_i / (2 pi) - band_low) / (band_high - band_low), 0, 1).
+ * Pair i is channels (i, i + rot_dim / 2), or with `interleaved` (2 i, 2 i + 1).  Channels from rot_dim
+ * on are copied.  Angles are taken in 64 bits, products in fp32.
+ */
+typedef struct moba_rope_shape {
+    int32_t batch, heads;  /* heads of Q                                                         */
+    int32_t kv_heads;      /* heads of K; 0 = heads                                              */
+    int32_t seqlen, head_dim;
+    int32_t q_rows, k_rows;         /* rows that a slice of Q / K takes in memory; 0 = seqlen    */
+    int32_t q_out_rows, k_out_rows; /* the same of Q_out and K_out, e.g. a cache the keys go to  */
+    int32_t dtype;         /* moba_dtype                                                         */
+    int32_t rot_dim;       /* even, <= head_dim; 0 = head_dim                                    */
+    int32_t interleaved;   /* 0 or 1                                                             */
+    double  theta;         /* > 0                                                                */
+    double  scale_factor;  /* > 0; 1 = none                                                      */
+    double  orig_len, band_low, band_high;   /* band_low < band_high where orig_len > 0          */
+    float   amplitude;     /* finite                                                             */
+    int64_t position0;     /* position of row r without `positions`: position0 + r; |.| <= 2^31  */
+} moba_rope_shape;
+
+/*
+ * Turns Q [b,heads,q_rows,d] and, unless K is NULL, K [b,kv,k_rows,d]: rows 0 .. seqlen - 1 of every
+ * slice, to the same rows of Q_out and K_out.  An output may be its input (then with the same rows per
+ * slice); otherwise no output overlaps an input or the other output.
+ *   positions  in   [b,seqlen] int32, or NULL
+ * moba_rope_backward maps gradients with respect to Q_out and K_out to those with respect to Q and K (the
+ * turn backwards, the same amplitude).  head_dim 64 or 128.  Pointers to tensors on 16-byte boundaries
+ * are the fast case; they must be aligned to an element (else MOBA_EINVAL).
+ */
+int moba_rope(const moba_rope_shape* shape, const void* Q, const void* K, const int32_t* positions,
+              void* Q_out, void* K_out, void* stream);
+int moba_rope_backward(const moba_rope_shape* shape, const void* dQ_out, const void* dK_out, const int32_t* positions,
+                       void* dQ, void* dK, void* stream);
+
+/*
  * moba_backward split into its kernels, for callers that time or overlap them:
  * `parts` is a bit set of MOBA_BWD_PREPROCESS (D = rowsum(dO o O) into the workspace),
  * MOBA_BWD_DQ and MOBA_BWD_DKDV (both read D from the workspace, so PREPROCESS must have

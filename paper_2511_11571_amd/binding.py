@@ -93,7 +93,8 @@ def lib():
         L.moba_last_hip_error.restype = ctypes.c_int
         for name in ("moba_routes_per_slice", "moba_workspace_bytes", "moba_centroids", "moba_topk",
                      "moba_topk_static", "moba_topk_varlen", "moba_varlen_layout", "moba_varlen_pad",
-                     "moba_varlen_unpad", "moba_varlen_block_first", "moba_build_lists", "moba_forward", "moba_backward", "moba_backward_parts",
+                     "moba_varlen_unpad", "moba_varlen_block_first", "moba_varlen_first_key", "moba_window_workspace",
+                     "moba_window_forward", "moba_window_backward", "moba_rope", "moba_rope_backward", "moba_build_lists", "moba_forward", "moba_backward", "moba_backward_parts",
                      "moba_decode_forward", "moba_decode_forward_ws", "moba_decode_workspace",
                      "moba_profile_begin", "moba_profile_end", "moba_key_conv_backward",
                      "moba_key_conv_backward_workspace", "moba_microbench_copy", "moba_microbench_mfma"):
@@ -253,6 +254,15 @@ class VarlenLayout:
                                        _stream()), name)
         return out
 
+    def first_key(self, padded=False):
+        """First key of the sequence of every row, [1, T] int32 ([1, T'] of the padded layout): what window_forward
+        and window_backward take for a packed batch."""
+        offs, n = (self.pad_offsets, self.padded_tokens) if padded else (self.seq_offsets, self.tokens)
+        out = torch.empty((1, n), dtype=torch.int32, device=offs.device)
+        _check(_fn("moba_varlen_first_key", "ipipp")(self.num_seqs, _p(offs), n, _p(out), _stream()),
+               "moba_varlen_first_key")
+        return out
+
     def pad(self, X):
         """[1, heads, T, ...] -> [1, heads, T', ...], zero rows after every sequence."""
         assert X.shape[2] == self.tokens
@@ -366,6 +376,181 @@ def decode_forward(shape: Shape, q_len, Q, K_eff, V, cent, want_idx=True):
                                      V.data_ptr(), _p(cent), blocks, O.data_ptr(), lse.data_ptr(), _p(idx), _p(ws), need,
                                      _stream()), "moba_decode_forward_ws")
     return O, lse, idx
+
+
+class _CWindowShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads", "kv_heads", "q_len", "kv_len", "kv_rows", "head_dim",
+                                              "window", "dtype")] + [("softmax_scale", ctypes.c_float)]
+
+
+class _CRopeShape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "heads", "kv_heads", "seqlen", "head_dim", "q_rows", "k_rows",
+                                               "q_out_rows", "k_out_rows", "dtype", "rot_dim", "interleaved")] +
+                [(n, ctypes.c_double) for n in ("theta", "scale_factor", "orig_len", "band_low", "band_high")] +
+                [("amplitude", ctypes.c_float), ("position0", ctypes.c_int64)])
+
+
+class _Struct:
+    """Shapes that the library takes as a C structure: built once per (immutable) object, as Shape._ref."""
+
+    def _ref(self):
+        s = self.__dict__.get("_cstruct")
+        if s is None:
+            s = self.__dict__.setdefault("_cstruct", self.c())
+        return ctypes.addressof(s)
+
+    @property
+    def hkv(self):
+        return self.kv_heads if self.kv_heads > 0 else self.heads
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.dtype == BF16 else torch.float32
+
+
+@dataclass(frozen=True)
+class WindowShape(_Struct):
+    """Causal attention of the last q_len of kv_len positions to the last ``window`` keys each (0: to all)."""
+    batch: int
+    heads: int
+    q_len: int
+    kv_len: int
+    head_dim: int
+    window: int = 0
+    dtype: int = BF16
+    softmax_scale: float = 0.0
+    kv_heads: int = 0          # grouped-query attention: key/value heads (0 = heads)
+    kv_rows: int = 0           # rows of a slice of K and V in memory (0 = kv_len)
+
+    def c(self):
+        return _CWindowShape(self.batch, self.heads, self.kv_heads, self.q_len, self.kv_len, self.kv_rows, self.head_dim,
+                             self.window, self.dtype, self.softmax_scale)
+
+    @property
+    def rows(self):
+        return self.kv_rows if self.kv_rows > 0 else self.kv_len
+
+
+@dataclass(frozen=True)
+class RopeShape(_Struct):
+    """Rotary positions (see moba_rope_shape in include/moba.h for the formulas).  Q has ``heads`` heads, K kv_heads."""
+    batch: int
+    heads: int
+    seqlen: int
+    head_dim: int
+    kv_heads: int = 0
+    dtype: int = BF16
+    rot_dim: int = 0           # channels that are turned (0 = head_dim)
+    interleaved: bool = False
+    theta: float = 10000.0
+    scale_factor: float = 1.0
+    orig_len: float = 0.0
+    band_low: float = 1.0
+    band_high: float = 32.0
+    amplitude: float = 1.0
+    position0: int = 0
+    q_rows: int = 0            # rows of a slice in memory (0 = seqlen)
+    k_rows: int = 0
+    q_out_rows: int = 0
+    k_out_rows: int = 0
+
+    def c(self):
+        return _CRopeShape(self.batch, self.heads, self.kv_heads, self.seqlen, self.head_dim, self.q_rows, self.k_rows,
+                           self.q_out_rows, self.k_out_rows, self.dtype, self.rot_dim, int(self.interleaved), self.theta,
+                           self.scale_factor, self.orig_len, self.band_low, self.band_high, self.amplitude, self.position0)
+
+
+def window_workspace_bytes(shape: WindowShape):
+    """-> bytes of window_forward's and of window_backward's workspace."""
+    n = shape.__dict__.get("_ws_bytes")      # a function of the (immutable) shape
+    if n is None:
+        a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        _check(_fn("moba_window_workspace", "ppp")(shape._ref(), ctypes.addressof(a), ctypes.addressof(b)),
+               "moba_window_workspace")
+        n = shape.__dict__.setdefault("_ws_bytes", (a.value, b.value))
+    return n
+
+
+def _window_args(shape, first_key, *tensors):
+    b, d, dt, dev = shape.batch, shape.head_dim, shape.torch_dtype, torch._C._cuda_getDevice()
+    for t, heads, rows in tensors:
+        assert t.is_contiguous() and t.dtype == dt and t.shape == (b, heads, rows, d) and t.get_device() == dev
+    if first_key is not None:
+        assert (first_key.is_contiguous() and first_key.dtype == torch.int32 and first_key.shape == (b, shape.q_len) and
+                first_key.get_device() == dev)
+
+
+def window_forward(shape: WindowShape, Q, K, V, first_key=None, ws=None, O=None, lse=None):
+    """-> (O [b,h,q_len,d], lse [b,h,q_len] fp32).  K, V: [b,kv,rows,d].  first_key: [b,q_len] int32, the first key
+    of the sequence that every row belongs to (VarlenLayout.first_key), or None."""
+    h, q = shape.heads, shape.q_len
+    _window_args(shape, first_key, (Q, h, q), (K, shape.hkv, shape.rows), (V, shape.hkv, shape.rows))
+    if O is None:
+        O = torch.empty_like(Q)
+    if lse is None:
+        lse = Q.new_empty(Q.shape[:3], dtype=torch.float32)
+    if ws is None:
+        need = window_workspace_bytes(shape)[0]
+        ws = _ws(need, Q) if need else None
+    assert lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == Q.shape[:3] and lse.device == Q.device
+    _window_args(shape, None, (O, h, q))
+    assert ws is None or (ws.is_contiguous() and ws.dtype == torch.uint8 and ws.device == Q.device)
+    _check(_fn("moba_window_forward", "p" * 8 + "zp")(shape._ref(), Q.data_ptr(), K.data_ptr(), V.data_ptr(), _p(first_key),
+                                                    O.data_ptr(), lse.data_ptr(), _p(ws),
+                                                    0 if ws is None else ws.numel(), _stream()), "moba_window_forward")
+    return O, lse
+
+
+def window_backward(shape: WindowShape, Q, K, V, O, lse, dO, first_key=None, ws=None, out=None):
+    """-> (dQ [b,h,q_len,d], dK, dV [b,kv,rows,d]).  Rows of dK and dV from kv_len on are not written."""
+    h, q, hkv, rows = shape.heads, shape.q_len, shape.hkv, shape.rows
+    _window_args(shape, first_key, (Q, h, q), (K, hkv, rows), (V, hkv, rows), (O, h, q), (dO, h, q))
+    assert lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == Q.shape[:3] and lse.device == Q.device
+    dQ, dK, dV = out if out is not None else (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V))
+    _window_args(shape, None, (dQ, h, q), (dK, hkv, rows), (dV, hkv, rows))
+    if ws is None:
+        ws = _ws(window_workspace_bytes(shape)[1], Q)
+    assert ws.is_contiguous() and ws.dtype == torch.uint8 and ws.device == Q.device
+    _check(_fn("moba_window_backward", "p" * 12 + "zp")(
+        shape._ref(), Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
+        _p(first_key), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
+        "moba_window_backward")
+    return dQ, dK, dV
+
+
+def _rope(name, shape, Q, K, positions, out):
+    b, n, d, dt, dev = shape.batch, shape.seqlen, shape.head_dim, shape.torch_dtype, torch._C._cuda_getDevice()
+    Qo, Ko = out if out is not None else (None, None)
+    if Qo is None:
+        Qo = Q.new_empty((b, shape.heads, shape.q_out_rows or n, d))
+    if Ko is None and K is not None:
+        Ko = K.new_empty((b, shape.hkv, shape.k_out_rows or n, d))
+    for t, heads, rows in ((Q, shape.heads, shape.q_rows), (Qo, shape.heads, shape.q_out_rows),
+                           (K, shape.hkv, shape.k_rows), (Ko, shape.hkv, shape.k_out_rows)):
+        # (a stretch of a cache's rows is a view with the cache's own stride)
+        if t is not None:
+            rows = rows or n
+            size, st = t.shape, t.stride()
+            assert t.dtype == dt and t.dim() == 4 and size[:2] == (b, heads) and size[3] == d and t.get_device() == dev
+            assert n <= size[2] <= rows and st[3] == 1 and (size[2] == 1 or st[2] == d)
+            assert (heads == 1 or st[1] == rows * d) and (b == 1 or st[0] == heads * rows * d)
+    if positions is not None:
+        assert (positions.is_contiguous() and positions.dtype == torch.int32 and positions.shape == (b, n) and
+                positions.get_device() == dev)
+    _check(_fn(name, "ppppppp")(shape._ref(), Q.data_ptr(), _p(K), _p(positions), Qo.data_ptr(), _p(Ko), _stream()), name)
+    return Qo, Ko
+
+
+def rope(shape: RopeShape, Q, K=None, positions=None, out=None):
+    """Turns Q [b,h,N,d] and K [b,kv,N,d] (or Q alone) by their positions -> (Q, K or None).  positions: [b,N] int32,
+    or None for position0, position0 + 1, ...  out = (Q_out, K_out) may be the inputs themselves, or views of N rows of
+    larger tensors with the shape's q_out_rows / k_out_rows rows per slice (a cache)."""
+    return _rope("moba_rope", shape, Q, K, positions, out)
+
+
+def rope_backward(shape: RopeShape, dQ, dK=None, positions=None, out=None):
+    """Gradients with respect to rope's results -> gradients with respect to its arguments."""
+    return _rope("moba_rope_backward", shape, dQ, dK, positions, out)
 
 
 PROFILE_KERNELS = ("topk", "forward", "bwd_dq", "bwd_dkdv")

@@ -263,6 +263,7 @@ hipError_t launch_varlen_copy(bool pad, const int32_t* seq_off, const int32_t* p
                               void* dst, hipStream_t st);
 hipError_t launch_varlen_block_first(const int32_t* pad_off, int num_seqs, int B, int nblocks, int32_t* first,
                                      hipStream_t st);
+hipError_t launch_varlen_first_key(const int32_t* offs, int num_seqs, int tokens, int32_t* first, hipStream_t st);
 hipError_t launch_topk_reference(const Dims& s, const void* Q, const float* cent, int32_t* idx,
                                  hipStream_t st);
 hipError_t launch_build_lists(const Dims& s, const int32_t* idx, int32_t* off, int32_t* ql,

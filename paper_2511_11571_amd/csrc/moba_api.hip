@@ -3,11 +3,14 @@
 // exercised on a machine without a GPU.
 #include <math.h>
 
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <utility>
 
 #include "mfma.h"
+#include "rope.h"
+#include "window.h"
 
 using namespace moba;
 
@@ -184,6 +187,116 @@ void* static_scratch(hipError_t* err)
     }
     return g_scratch_ptr[dev];
 }
+}  // namespace
+
+// ---- layers beside MoBA: sliding-window attention and rotary positions ----------------------
+namespace {
+
+bool aligned(uintptr_t to, std::initializer_list<const void*> ps)
+{
+    uintptr_t all = 0;
+    for (const void* p : ps) all |= reinterpret_cast<uintptr_t>(p);
+    return all % to == 0;
+}
+
+int make_window_dims(const moba_window_shape* sh, WindowDims& d)
+{
+    if (!sh) return MOBA_EINVAL;
+    if (sh->batch <= 0 || sh->heads <= 0 || sh->kv_heads < 0 || sh->head_dim <= 0) return MOBA_EINVAL;
+    if (sh->kv_heads > 0 && sh->heads % sh->kv_heads != 0) return MOBA_EINVAL;
+    if (sh->q_len <= 0 || sh->kv_len < sh->q_len || sh->window < 0) return MOBA_EINVAL;
+    if (sh->kv_rows != 0 && sh->kv_rows < sh->kv_len) return MOBA_EINVAL;
+    if (sh->dtype != MOBA_F32 && sh->dtype != MOBA_BF16) return MOBA_EINVAL;
+    if (!(sh->softmax_scale == sh->softmax_scale) || isinf(sh->softmax_scale)) return MOBA_EINVAL;
+    if (sh->head_dim != 64 && sh->head_dim != 128) return MOBA_EUNSUPPORTED;
+    if (sh->kv_len > kMaxSeqlen || sh->kv_rows > kMaxSeqlen) return MOBA_EUNSUPPORTED;
+    if ((int64_t)sh->batch * sh->heads > 65535) return MOBA_EUNSUPPORTED;
+    d.batch = sh->batch;
+    d.heads = sh->heads;
+    d.hkv = sh->kv_heads > 0 ? sh->kv_heads : sh->heads;
+    d.G = d.heads / d.hkv;
+    d.bh = d.batch * d.heads;
+    d.bhk = d.batch * d.hkv;
+    d.q = sh->q_len;
+    d.N = sh->kv_len;
+    d.rows = sh->kv_rows > 0 ? sh->kv_rows : sh->kv_len;
+    d.D = sh->head_dim;
+    d.W = sh->window == 0 || sh->window > sh->kv_len ? sh->kv_len : sh->window;
+    d.dtype = sh->dtype;
+    d.scale = sh->softmax_scale > 0.f ? sh->softmax_scale : 1.0f / sqrtf((float)d.D);
+    return MOBA_OK;
+}
+
+int rope_args(const moba_rope_shape* sh, RopeArgs& a)
+{
+    if (!sh) return MOBA_EINVAL;
+    if (sh->batch <= 0 || sh->heads <= 0 || sh->kv_heads < 0 || sh->seqlen <= 0 || sh->head_dim <= 0) return MOBA_EINVAL;
+    for (const int32_t rows : {sh->q_rows, sh->k_rows, sh->q_out_rows, sh->k_out_rows})
+        if (rows != 0 && rows < sh->seqlen) return MOBA_EINVAL;
+    if (sh->dtype != MOBA_F32 && sh->dtype != MOBA_BF16) return MOBA_EINVAL;
+    if (sh->rot_dim < 0 || sh->rot_dim > sh->head_dim || sh->rot_dim % 2 != 0) return MOBA_EINVAL;
+    if (sh->interleaved != 0 && sh->interleaved != 1) return MOBA_EINVAL;
+    if (!(sh->theta > 0.0) || isinf(sh->theta) || !(sh->scale_factor > 0.0) || isinf(sh->scale_factor)) return MOBA_EINVAL;
+    if (!(sh->orig_len >= 0.0) || isinf(sh->orig_len)) return MOBA_EINVAL;
+    if (sh->orig_len > 0.0 && (!(sh->band_low < sh->band_high) || isinf(sh->band_low) || isinf(sh->band_high)))
+        return MOBA_EINVAL;
+    if (!(sh->amplitude == sh->amplitude) || isinf(sh->amplitude)) return MOBA_EINVAL;
+    if (sh->position0 > ((int64_t)1 << 31) || sh->position0 < -((int64_t)1 << 31)) return MOBA_EINVAL;
+    if (sh->head_dim != 64 && sh->head_dim != 128) return MOBA_EUNSUPPORTED;
+    if (sh->seqlen > kMaxSeqlen || sh->q_rows > kMaxSeqlen || sh->k_rows > kMaxSeqlen || sh->q_out_rows > kMaxSeqlen ||
+        sh->k_out_rows > kMaxSeqlen)
+        return MOBA_EUNSUPPORTED;
+    if ((int64_t)sh->batch * sh->heads > 65535 || (int64_t)sh->batch * sh->kv_heads > 65535) return MOBA_EUNSUPPORTED;
+    a.batch = sh->batch;
+    a.N = sh->seqlen;
+    a.D = sh->head_dim;
+    a.rot = sh->rot_dim > 0 ? sh->rot_dim : sh->head_dim;
+    a.interleaved = sh->interleaved;
+    a.dtype = sh->dtype;
+    a.amp = sh->amplitude;
+    a.pos0 = sh->position0;
+    a.heads[0] = sh->heads;
+    a.heads[1] = sh->kv_heads > 0 ? sh->kv_heads : sh->heads;
+    auto rows = [&](int32_t r) { return r > 0 ? r : sh->seqlen; };
+    a.xrows[0] = rows(sh->q_rows);
+    a.xrows[1] = rows(sh->k_rows);
+    a.yrows[0] = rows(sh->q_out_rows);
+    a.yrows[1] = rows(sh->k_out_rows);
+    const double two_pi = 6.283185307179586476925;
+    for (int i = 0; i < a.rot / 2; ++i) {
+        double f = pow(sh->theta, -2.0 * i / a.rot);
+        if (sh->scale_factor != 1.0) {
+            double keep = 0.0;
+            if (sh->orig_len > 0.0) {
+                keep = (sh->orig_len * f / two_pi - sh->band_low) / (sh->band_high - sh->band_low);
+                keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            }
+            f *= keep + (1.0 - keep) / sh->scale_factor;
+        }
+        a.freq[i] = f / two_pi;
+    }
+    return MOBA_OK;
+}
+
+int run_rope(const moba_rope_shape* shape, float sign, const void* Q, const void* K, const int32_t* positions, void* Qo,
+             void* Ko, void* stream)
+{
+    RopeArgs a;
+    const int st = rope_args(shape, a);
+    if (st != MOBA_OK) return st;
+    if (!Q || !Qo || !K != !Ko) return MOBA_EINVAL;
+    if ((Q == Qo && a.xrows[0] != a.yrows[0]) || (K && K == Ko && a.xrows[1] != a.yrows[1])) return MOBA_EINVAL;
+    if (!aligned(a.dtype == MOBA_BF16 ? 2 : 4, {Q, K, Qo, Ko}) || !aligned(4, {positions})) return MOBA_EINVAL;
+    a.x[0] = Q;
+    a.y[0] = Qo;
+    a.x[1] = K;
+    a.y[1] = Ko;
+    if (!K) a.heads[1] = 0;
+    a.pos = positions;
+    a.sign = sign;
+    return hip_status(launch_rope(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -478,6 +591,61 @@ int moba_decode_forward(const moba_shape* shape, int32_t q_len, const void* Q, c
 {
     return moba_decode_forward_ws(shape, q_len, Q, K_eff, V, centroids, centroid_blocks, O, lse, topk_idx, nullptr, 0,
                                   stream);
+}
+
+int moba_window_workspace(const moba_window_shape* shape, size_t* fwd_ws, size_t* bwd_ws)
+{
+    WindowDims d;
+    const int st = make_window_dims(shape, d);
+    if (st != MOBA_OK) return st;
+    if (!fwd_ws || !bwd_ws) return MOBA_EINVAL;
+    *fwd_ws = window_forward_ws_bytes(d);
+    *bwd_ws = window_backward_ws_bytes(d);
+    return MOBA_OK;
+}
+
+int moba_window_forward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,
+                        const int32_t* first_key, void* O, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    WindowDims d;
+    const int st = make_window_dims(shape, d);
+    if (st != MOBA_OK) return st;
+    if (!Q || !K || !V || !O || !lse) return MOBA_EINVAL;
+    if (!aligned(16, {Q, K, V, O, ws}) || !aligned(4, {first_key, lse})) return MOBA_EINVAL;
+    const size_t need = window_forward_ws_bytes(d);
+    if (need > 0 && (!ws || ws_bytes < need)) return MOBA_EWORKSPACE;
+    return hip_status(launch_window_forward(d, Q, K, V, first_key, O, lse, ws, (hipStream_t)stream));
+}
+
+int moba_window_backward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,
+                         const void* O, const float* lse, const void* dO, const int32_t* first_key,
+                         void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes, void* stream)
+{
+    WindowDims d;
+    const int st = make_window_dims(shape, d);
+    if (st != MOBA_OK) return st;
+    if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV) return MOBA_EINVAL;
+    if (!aligned(16, {Q, K, V, O, dO, dQ, dK, dV, ws}) || !aligned(4, {first_key, lse})) return MOBA_EINVAL;
+    if (!ws || ws_bytes < window_backward_ws_bytes(d)) return MOBA_EWORKSPACE;
+    return hip_status(launch_window_backward(d, Q, K, V, O, lse, dO, first_key, dQ, dK, dV, ws, (hipStream_t)stream));
+}
+
+int moba_varlen_first_key(int32_t num_seqs, const int32_t* offsets, int32_t tokens, int32_t* first_key, void* stream)
+{
+    if (num_seqs <= 0 || tokens < 0 || !offsets || (tokens > 0 && !first_key)) return MOBA_EINVAL;
+    return hip_status(launch_varlen_first_key(offsets, num_seqs, tokens, first_key, (hipStream_t)stream));
+}
+
+int moba_rope(const moba_rope_shape* shape, const void* Q, const void* K, const int32_t* positions,
+              void* Q_out, void* K_out, void* stream)
+{
+    return run_rope(shape, 1.f, Q, K, positions, Q_out, K_out, stream);
+}
+
+int moba_rope_backward(const moba_rope_shape* shape, const void* dQ_out, const void* dK_out, const int32_t* positions,
+                       void* dQ, void* dK, void* stream)
+{
+    return run_rope(shape, -1.f, dQ_out, dK_out, positions, dQ, dK, stream);
 }
 
 int moba_backward_parts(const moba_shape* shape, const void* Q, const void* K_eff, const void* V,

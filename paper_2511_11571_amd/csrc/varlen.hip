@@ -59,6 +59,15 @@ __global__ __launch_bounds__(256) void varlen_block_first_kernel(const int32_t* 
     first[c] = pad_off[seq_of(pad_off, num_seqs, c * B)] / B;
 }
 
+// start of the sequence that every row belongs to; rows behind the last sequence are not written
+__global__ __launch_bounds__(256) void varlen_first_key_kernel(const int32_t* __restrict__ offs, int num_seqs,
+                                                               int tokens, int32_t* __restrict__ first)
+{
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= min(tokens, offs[num_seqs])) return;
+    first[t] = offs[seq_of(offs, num_seqs, t)];
+}
+
 template <typename T>
 static hipError_t varlen_copy_launch(bool pad, const int32_t* seq_off, const int32_t* pad_off, int num_seqs,
                                      int64_t slices, int tokens, int padded_tokens, int row_elems,
@@ -94,6 +103,14 @@ hipError_t launch_varlen_block_first(const int32_t* pad_off, int num_seqs, int B
     if (nblocks == 0) return hipSuccess;
     hipLaunchKernelGGL(varlen_block_first_kernel, dim3((nblocks + 255) / 256), dim3(256), 0, st, pad_off,
                        num_seqs, B, nblocks, first);
+    return hipGetLastError();
+}
+
+hipError_t launch_varlen_first_key(const int32_t* offs, int num_seqs, int tokens, int32_t* first, hipStream_t st)
+{
+    if (tokens == 0) return hipSuccess;
+    hipLaunchKernelGGL(varlen_first_key_kernel, dim3((unsigned)((tokens + 255ll) / 256)), dim3(256), 0, st, offs,
+                       num_seqs, tokens, first);
     return hipGetLastError();
 }
 
