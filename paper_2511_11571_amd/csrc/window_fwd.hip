@@ -1,25 +1,201 @@
-// Causal attention to the last W keys: forward.  A wave per row.
-#include "window.h"
+// Causal attention to the last W keys: forward.
+//
+// A workgroup takes a tile of neighbouring queries of one head, a wave 32 CT of them, and walks the keys that
+// some of them attend in tiles of KT rows through LDS; the next tile is on its way from memory meanwhile.  Scores
+// are computed transposed, S^T = K Q^T, so that a lane holds a query's scores of half the keys and the softmax's
+// maximum and sum cost one exchange of halves; O^T = V^T P^T takes P as it comes out.  Statistics and sums
+// are fp32; P enters its product in the I/O type.
+//
+// The reference m of a row's exponents follows its maximum only when that has grown by more than 2^8: P stays
+// below 2^8, and most tiles scale nothing.
+#include "window_tiles.h"
 
 namespace moba {
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
-                                                             const T* __restrict__ V, T* __restrict__ O,
-                                                             float* __restrict__ lse)
+template <typename T, int D, int CT, int NW, int KT>
+__global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
+                                                                   const T* __restrict__ K, const T* __restrict__ V,
+                                                                   T* __restrict__ O, float* __restrict__ lse, int ntiles)
 {
-    const int r = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (r < a.q) plain_forward_row<T, D>(a, Q, K, V, O, lse, blockIdx.y, r, threadIdx.x % kWave);
+    constexpr int NT = NW * kWave, QT = 32 * CT * NW, STEPS = D / 16, MT = D / 32;
+    using KV = Tile<T, D, KT>;
+    extern __shared__ __align__(16) unsigned char smem[];    // K, V | K, V
+    __shared__ int wg_lo[NW];
+    const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    int skv, pos;
+    if (!schedule(blockIdx.x, a.bhk, a.G * ntiles, skv, pos)) return;
+    const int tile = ntiles - 1 - pos / a.G, s = skv * a.G + pos % a.G;      // the longest rows first
+    const T* Ks = K + (int64_t)skv * a.rows * D;
+    const T* Vs = V + (int64_t)skv * a.rows * D;
+    const int t0 = a.N - a.q, r0 = tile * QT + wave * 32 * CT;
+    int lo[CT], t[CT];
+    Opnd<T> q[CT][STEPS];
+    int lo_min = 0x7fffffff, lo_max = 0;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int r = min(r0 + 32 * c + m32, a.q - 1);       // (rows past the end: the last one again, not stored)
+        t[c] = t0 + r;
+        lo[c] = window_first(a, s, r);
+        if (lo[c] <= t[c]) lo_min = min(lo_min, lo[c]);
+        lo_max = max(lo_max, lo[c]);
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) load_opnd(q[c][e], Q + ((int64_t)s * a.q + r) * D + 16 * e + 8 * h);
+    }
+    // keys of the wave's rows: from lo_min to t_max, all rows attend those from lo_max to t_min
+    lo_min = r0 < a.q ? wave_min_i(lo_min) : 0x7fffffff;
+    lo_max = wave_max_i(lo_max);
+    const int t_min = t0 + min(r0, a.q - 1), t_max = t0 + min(r0 + 32 * CT - 1, a.q - 1);
+    if (lane == 0) wg_lo[wave] = lo_min;
+    __syncthreads();
+    int begin = wg_lo[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
+    begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
+    const int end = t0 + min((tile + 1) * QT, a.q);          // (begin beyond it: nobody attends anything)
+
+    const float c2 = a.scale * kLog2e;
+    f32x16_t acc[CT][MT];
+    float ref[CT], l[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        ref[c] = kLowest;
+        l[c] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[c][mt] = f32x16_t{};
+    }
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, auto edge) {
+        f32x16_t S[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) S[c] = f32x16_t{};
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) {
+            Opnd<T> k;
+            KV::rows(k, kt, row0, e, h, m32);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) S[c] = mma(k, q[c][e], S[c]);
+        }
+        Opnd<T> p[CT][2];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = S[c][i];
+                if constexpr (decltype(edge)::value) {
+                    const int key = u + result_row(i) + 4 * h;
+                    x[i] = key <= t[c] && key >= lo[c] ? x[i] : -INFINITY;
+                }
+            }
+            float top = x[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
+            top = max_halves(top) * c2;
+            if (__ballot(top > ref[c] + 8.f)) {
+                const float now = fmaxf(ref[c], top), alpha = fast_exp2(ref[c] - now);
+                ref[c] = now;
+                l[c] *= alpha;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) acc[c][mt] *= alpha;
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = fast_exp2(fmaf(x[i], c2, -ref[c]));
+                sum += x[i];
+            }
+            l[c] += sum;
+            pack_opnd(p[c][0], x);
+            pack_opnd(p[c][1], x + 8);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                Opnd<T> v;
+                KV::cols(v, vt, row0 + 16 * j, mt, lane);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[c][mt] = mma(v, p[c][j], acc[c][mt]);
+            }
+    };
+    if (begin < end) {
+        typename KV::template Moved<NT> mk, mv;
+        mk.load(Ks, begin, a.N - 1, tid);
+        mv.load(Vs, begin, a.N - 1, tid);
+        mk.store(smem, tid);
+        mv.store(smem + KV::BYTES, tid);
+        __syncthreads();
+        int buf = 0;
+        for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
+            const bool more = u0 + KT < end;
+            if (more) {
+                mk.load(Ks, u0 + KT, a.N - 1, tid);
+                mv.load(Vs, u0 + KT, a.N - 1, tid);
+            }
+            const unsigned char* kt = smem + buf * 2 * KV::BYTES;
+#pragma unroll
+            for (int x = 0; x < KT / 32; ++x) {
+                const int u = u0 + 32 * x;
+                if (u > t_max || u + 31 < lo_min) continue;
+                if (u + 31 <= t_min && u >= lo_max) keys32(kt, kt + KV::BYTES, 32 * x, u, std::false_type());
+                else keys32(kt, kt + KV::BYTES, 32 * x, u, std::true_type());
+            }
+            if (more) {
+                unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+                mk.store(to, tid);
+                mv.store(to + KV::BYTES, tid);
+            }
+            __syncthreads();
+        }
+    }
+    if (r0 >= a.q) return;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int r = r0 + 32 * c + m32;
+        const int64_t row = (int64_t)s * a.q + r;
+        const bool empty = lo[c] > t[c];
+        const float L = sum_halves(l[c]), inv = empty ? 0.f : 1.f / L;
+        bool odd = false;                                    // a result that is not finite
+        if (r < a.q) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    float o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        o[e] = empty ? 0.f : acc[c][mt][i + e] * inv;
+                        odd |= !(fabsf(o[e]) < INFINITY);
+                    }
+                    T* to = O + row * D + 32 * mt + result_row(i) + 4 * h;
+                    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+                    else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+                }
+            if (h == 0) lse[row] = empty ? -INFINITY : (ref[c] + fast_log2(L)) * kLn2;
+        }
+        // A weight of zero does not hide an infinity or a NaN: such rows are done once more, from their own pairs alone
+        uint64_t bad = __ballot(odd);
+        bad = (bad | bad >> 32) & 0xffffffffu;
+        for (; bad; bad &= bad - 1) plain_forward_row<T, D>(a, Q, K, V, O, lse, s, r0 + 32 * c + __builtin_ctzll(bad), lane);
+    }
 }
 
 size_t window_forward_ws_bytes(const WindowDims&) { return 0; }
 
-template <typename T, int D>
-static hipError_t forward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
-                            void* O, float* lse, hipStream_t st)
+template <typename T, int D, int CT, int NW, int KT>
+static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
+                          void* O, float* lse, hipStream_t st)
 {
-    hipLaunchKernelGGL((window_forward_kernel<T, D>), dim3((s.q + 3) / 4, s.bh), dim3(256), 0, st, window_args(s, first),
-                       (const T*)Q, (const T*)K, (const T*)V, (T*)O, lse);
+    auto* kernel = window_forward_kernel<T, D, CT, NW, KT>;
+    constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
+    if (lds > 64 * 1024) {
+        const hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
+        if (e != hipSuccess) return e;
+    }
+    constexpr int QT = 32 * CT * NW;
+    const int ntiles = (s.q + QT - 1) / QT;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, s.G * ntiles)), dim3(NW * kWave), lds, st,
+                       window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (T*)O, lse, ntiles);
     return hipGetLastError();
 }
 
@@ -27,10 +203,10 @@ hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void*
                                  void* O, float* lse, void*, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? forward_t<bf16_t, 64>(s, Q, K, V, first, O, lse, st)
-                         : forward_t<bf16_t, 128>(s, Q, K, V, first, O, lse, st);
-    return s.D == 64 ? forward_t<float, 64>(s, Q, K, V, first, O, lse, st)
-                     : forward_t<float, 128>(s, Q, K, V, first, O, lse, st);
+        return s.D == 64 ? tiles_t<bf16_t, 64, 1, 4, 64>(s, Q, K, V, first, O, lse, st)
+                         : tiles_t<bf16_t, 128, 1, 4, 64>(s, Q, K, V, first, O, lse, st);
+    return s.D == 64 ? tiles_t<float, 64, 1, 4, 32>(s, Q, K, V, first, O, lse, st)
+                     : tiles_t<float, 128, 1, 4, 32>(s, Q, K, V, first, O, lse, st);
 }
 
 }  // namespace moba

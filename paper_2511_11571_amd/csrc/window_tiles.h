@@ -1,0 +1,121 @@
+// Operands of the 32 x 32 matrix products of the window-attention kernels, for bf16 and fp32 alike.
+//
+// A step of a product contracts 16 slots.  With lane = 32 h + m, an operand holds row (or column) m, slots
+// 8 h .. 8 h + 7: one v_mfma_f32_32x32x16_bf16, or eight v_mfma_f32_32x32x2_f32 of which the s-th contracts
+// slots s and 8 + s.  Result element i of a lane is row 8 (i >> 2) + 4 h + (i & 3) of column m.  Elements
+// 8 j .. 8 j + 7 of a result are therefore the second operand of step j of a product over its rows, whose slot
+// 8 h + s is row 16 j + 8 (s >> 2) + 4 h + (s & 3): probabilities never change lanes.
+//
+// Tiles of rows lie in LDS row by row, the 16-byte pieces of row r at places exchanged by r & 7: rows read as
+// operands (a piece of 32 rows at once) and columns (four rows by sixteen channels at once) both use all banks.
+#pragma once
+#include "window.h"
+
+namespace moba {
+
+template <typename T> struct Opnd;
+template <> struct Opnd<bf16_t> { Frag f; };
+template <> struct Opnd<float> { float v[8]; };
+
+__device__ __forceinline__ f32x16_t mma(const Opnd<bf16_t>& a, const Opnd<bf16_t>& b, f32x16_t c) { return mfma32(a.f, b.f, c); }
+__device__ __forceinline__ f32x16_t mma(const Opnd<float>& a, const Opnd<float>& b, f32x16_t c)
+{
+#pragma unroll
+    for (int s = 0; s < 8; ++s) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[s], b.v[s], c, 0, 0, 0);
+    return c;
+}
+
+// eight neighbouring elements of a row in memory
+__device__ __forceinline__ void load_opnd(Opnd<bf16_t>& o, const bf16_t* p) { o.f.q = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void load_opnd(Opnd<float>& o, const float* p) { Vec8<float>::load(p, o.v); }
+
+// eight elements of a result
+__device__ __forceinline__ void pack_opnd(Opnd<bf16_t>& o, const float* p)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o.f.u[e] = pack2(p[2 * e], p[2 * e + 1]);
+}
+__device__ __forceinline__ void pack_opnd(Opnd<float>& o, const float* p)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = p[e];
+}
+
+// A tile of ROWS rows of D channels in LDS
+template <typename T, int D, int ROWS>
+struct Tile {
+    static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, BYTES = ROWS * RB;
+
+    // what a workgroup of NT threads moves from memory to LDS: PER pieces of every thread
+    template <int NT>
+    struct Moved {
+        static constexpr int PER = ROWS * PIECES / NT;
+        static_assert(ROWS * PIECES % NT == 0, "whole pieces");
+        uint4 x[PER];
+        // rows first .. first + ROWS of a slice, rows from last + 1 on replaced by row `last`
+        __device__ __forceinline__ void load(const T* __restrict__ slice, int first, int last, int tid)
+        {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int id = tid + i * NT, row = min(first + id / PIECES, last);
+                x[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(slice) + (int64_t)row * RB + 16 * (id % PIECES));
+            }
+        }
+        __device__ __forceinline__ void store(unsigned char* tile, int tid) const
+        {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int id = tid + i * NT, row = id / PIECES;
+                *reinterpret_cast<uint4*>(tile + row * RB + 16 * ((id % PIECES) ^ (row & 7))) = x[i];
+            }
+        }
+    };
+
+    // rows row0 + m, channels 16 c + 8 h .. + 7 (row0 a multiple of 8)
+    static __device__ __forceinline__ void rows(Opnd<T>& o, const unsigned char* tile, int row0, int c, int h, int m)
+    {
+        const unsigned char* p = tile + (row0 + m) * RB;
+        if constexpr (sizeof(T) == 2) {
+            o.f.q = *reinterpret_cast<const uint4*>(p + (16 * ((2 * c) ^ (h ^ (m & 7)))));
+        } else {
+            const float4 a = *reinterpret_cast<const float4*>(p + 16 * ((4 * c) ^ ((2 * h) ^ (m & 7))));
+            const float4 b = *reinterpret_cast<const float4*>(p + 16 * ((4 * c) ^ ((2 * h + 1) ^ (m & 7))));
+            o.v[0] = a.x; o.v[1] = a.y; o.v[2] = a.z; o.v[3] = a.w;
+            o.v[4] = b.x; o.v[5] = b.y; o.v[6] = b.z; o.v[7] = b.w;
+        }
+    }
+    // the transpose: channel 32 mt + m, slots in the order of a result's rows, of rows row0 .. row0 + 15
+    // (row0 a multiple of 8)
+    static __device__ __forceinline__ void cols(Opnd<T>& o, const unsigned char* tile, int row0, int mt, int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            const int e = (lane & 15) >> 2, q = lane & 3;
+            const unsigned char* p = tile + (row0 + 4 * h + e) * RB + ((64 * mt) ^ (16 * ((2 * ((lane >> 4) & 1) + (q >> 1)) ^ (4 * h + e)))) + 8 * (q & 1);
+            const uint2 a = lds_read_tr16(p), b = lds_read_tr16(p + 8 * RB);
+            o.f.u[0] = a.x; o.f.u[1] = a.y; o.f.u[2] = b.x; o.f.u[3] = b.y;
+        } else {
+            const int m = lane & 31;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const int r = 8 * (s >> 2) + 4 * h + (s & 3);
+                o.v[s] = *reinterpret_cast<const float*>(tile + (row0 + r) * RB + 128 * mt + 16 * ((m >> 2) ^ (r & 7)) + 4 * (m & 3));
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ int wave_min_i(int x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, kWave));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max_i(int x) { return -wave_min_i(-x); }
+
+// row of a result's element i
+__device__ __forceinline__ constexpr int result_row(int i) { return 8 * (i >> 2) + (i & 3); }
+
+constexpr float kLowest = -3.402823466e+38f;
+
+}  // namespace moba
