@@ -1,66 +1,355 @@
-// Causal attention to the last W keys: backward.  D = rowsum(dO o O), then a wave per row for dQ and a
-// wave per key for dK and dV.
-#include "window.h"
+// Causal attention to the last W keys: backward, which recomputes the probabilities P = exp(S - lse).
+//
+// Two kernels, no atomics, the same sums in every run:
+//   dQ by tiles of queries, as the forward walks: S^T = K Q^T and dP^T = V dO^T, dS = P o (dP - D), dQ^T += K^T dS^T.
+//     The rows' D = rowsum(dO o O) is taken here, from the operands at hand, and left for the other kernel;
+//   dK and dV by tiles of keys, a wave 32 of them, walking the queries that see them, all heads that share the
+//     keys one after the other: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+// Seven products for the five that are needed; one kernel for both would add dQ up by atomics or write partial
+// sums of it.  D enters as the start value of the dP product.
+#include "window_tiles.h"
 
 namespace moba {
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_rowdot_kernel(const T* __restrict__ O, const T* __restrict__ dO,
-                                                            float* __restrict__ Dv, int64_t rows)
+// what the dQ kernel leaves: D of every row and, with first keys, the smallest and largest of 32 rows each
+struct WindowLeft {
+    float* D;                   // [bh][q]
+    int2* lo;                   // [batch][ceil(q / 32)]; rows that attend nothing count as INT_MAX in the smallest
+};
+
+template <typename T, int D, int NW, int KT>
+__global__ __launch_bounds__(NW* kWave) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+                                                              const T* __restrict__ V, const T* __restrict__ O,
+                                                              const float* __restrict__ lse, const T* __restrict__ dO,
+                                                              T* __restrict__ dQ, WindowLeft left, int ntiles)
 {
-    constexpr int L = D / 8;                                 // lanes of a row
-    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    if (row >= rows) return;
-    float x[8], y[8], a = 0.f;
-    Vec8<T>::load(O + row * D + 8 * (threadIdx.x % L), x);
-    Vec8<T>::load(dO + row * D + 8 * (threadIdx.x % L), y);
+    constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
+    using KV = Tile<T, D, KT>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int wg_lo[NW];
+    const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    int skv, pos;
+    if (!schedule(blockIdx.x, a.bhk, a.G * ntiles, skv, pos)) return;
+    const int tile = ntiles - 1 - pos / a.G, s = skv * a.G + pos % a.G;
+    const T* Ks = K + (int64_t)skv * a.rows * D;
+    const T* Vs = V + (int64_t)skv * a.rows * D;
+    const int t0 = a.N - a.q, r0 = tile * QT + wave * 32;
+    const int r = min(r0 + m32, a.q - 1), t = t0 + r, lo = window_first(a, s, r);
+    const int64_t row = (int64_t)s * a.q + r;
+    Opnd<T> q[STEPS], g[STEPS];
+    float Dr = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a = fmaf(x[e], y[e], a);
+    for (int e = 0; e < STEPS; ++e) {
+        const int64_t at = row * D + 16 * e + 8 * h;
+        load_opnd(q[e], Q + at);
+        load_opnd(g[e], dO + at);
+        float x[8], y[8];
+        Vec8<T>::load(dO + at, x);
+        Vec8<T>::load(O + at, y);
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) a += __shfl_xor(a, o, L);
-    if (threadIdx.x % L == 0) Dv[row] = a;
+        for (int i = 0; i < 8; ++i) Dr = fmaf(x[i], y[i], Dr);
+    }
+    Dr = sum_halves(Dr);
+    const bool mine = r0 + m32 < a.q;
+    if (mine && h == 0) left.D[row] = Dr;
+    const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
+    const int lo_min = r0 < a.q ? wave_min_i(lo <= t ? lo : 0x7fffffff) : 0x7fffffff, lo_max = wave_max_i(lo);
+    const int t_min = t0 + min(r0, a.q - 1), t_max = t0 + min(r0 + 31, a.q - 1);
+    if (lane == 0) {
+        wg_lo[wave] = lo_min;
+        if (left.lo && s % a.heads == 0 && r0 < a.q) left.lo[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(lo_min, lo_max);
+    }
+    __syncthreads();
+    int begin = wg_lo[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
+    begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
+    const int end = t0 + min((tile + 1) * QT, a.q);
+
+    f32x16_t acc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, auto edge) {
+        f32x16_t S = f32x16_t{}, dP;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dP[i] = -Dr;
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) {
+            Opnd<T> k, v;
+            KV::rows(k, kt, row0, e, h, m32);
+            S = mma(k, q[e], S);
+            KV::rows(v, vt, row0, e, h, m32);
+            dP = mma(v, g[e], dP);
+        }
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
+            if constexpr (decltype(edge)::value) {
+                const int key = u + result_row(i) + 4 * h;
+                x[i] = key <= t && key >= lo ? x[i] : 0.f;
+            }
+        }
+        Opnd<T> p[2];
+        pack_opnd(p[0], x);
+        pack_opnd(p[1], x + 8);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                Opnd<T> k;
+                KV::cols(k, kt, row0 + 16 * j, mt, lane);
+                acc[mt] = mma(k, p[j], acc[mt]);
+            }
+    };
+    if (begin < end) {
+        typename KV::template Moved<NT> mk, mv;
+        mk.load(Ks, begin, a.N - 1, tid);
+        mv.load(Vs, begin, a.N - 1, tid);
+        mk.store(smem, tid);
+        mv.store(smem + KV::BYTES, tid);
+        __syncthreads();
+        int buf = 0;
+        for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
+            const bool more = u0 + KT < end;
+            if (more) {
+                mk.load(Ks, u0 + KT, a.N - 1, tid);
+                mv.load(Vs, u0 + KT, a.N - 1, tid);
+            }
+            const unsigned char* kt = smem + buf * 2 * KV::BYTES;
+#pragma unroll
+            for (int x = 0; x < KT / 32; ++x) {
+                const int u = u0 + 32 * x;
+                if (u > t_max || u + 31 < lo_min) continue;
+                if (u + 31 <= t_min && u >= lo_max) keys32(kt, kt + KV::BYTES, 32 * x, u, std::false_type());
+                else keys32(kt, kt + KV::BYTES, 32 * x, u, std::true_type());
+            }
+            if (more) {
+                unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+                mk.store(to, tid);
+                mv.store(to + KV::BYTES, tid);
+            }
+            __syncthreads();
+        }
+    }
+    bool odd = false;
+    if (mine) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                float o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = lo > t ? 0.f : acc[mt][i + e] * a.scale;
+                    odd |= !(fabsf(o[e]) < INFINITY);
+                }
+                T* to = dQ + row * D + 32 * mt + result_row(i) + 4 * h;
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+                else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+            }
+    }
+    // rows with a sum that is not finite once more, from their own pairs alone
+    uint64_t bad = __ballot(odd);
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, left.D, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
-                                                        const T* __restrict__ V, const T* __restrict__ dO,
-                                                        const float* __restrict__ lse, const float* __restrict__ Dv,
-                                                        T* __restrict__ dQ)
+template <typename T, int D, int NW, int QT>
+__global__ __launch_bounds__(NW* kWave) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+                                                                const T* __restrict__ V, const float* __restrict__ lse,
+                                                                const T* __restrict__ dO, T* __restrict__ dK,
+                                                                T* __restrict__ dV, WindowLeft left, int ntiles)
 {
-    const int r = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (r < a.q) plain_dq_row<T, D>(a, Q, K, V, dO, lse, Dv, dQ, blockIdx.y, r, threadIdx.x % kWave);
+    constexpr int NT = NW * kWave, KTILE = 32 * NW, STEPS = D / 16, MT = D / 32;
+    static_assert(QT <= kWave, "a lane per row of a tile");
+    using QG = Tile<T, D, QT>;
+    extern __shared__ __align__(16) unsigned char smem[];    // Q, dO | Q, dO
+    __shared__ __align__(16) float stat_z[2][QT], stat_d[2][QT];             // -lse (log2 units), -D
+    __shared__ int stat_lo[2][QT], range[NW];
+    const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    int skv, tile;
+    if (!schedule(blockIdx.x, a.bhk, ntiles, skv, tile)) return;             // (the first keys have the most queries)
+    const int t0 = a.N - a.q, k0 = tile * KTILE, ku = k0 + wave * 32, key = ku + m32;
+    Opnd<T> k[STEPS], v[STEPS];
+    {
+        const int64_t at = ((int64_t)skv * a.rows + min(key, a.N - 1)) * D;  // (keys past the end: the last one, not stored)
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) {
+            load_opnd(k[e], K + at + 16 * e + 8 * h);
+            load_opnd(v[e], V + at + 16 * e + 8 * h);
+        }
+    }
+    const float c2 = a.scale * kLog2e;
+    // rows that may see a key of the workgroup: from the first key's own on, to the last key's last one
+    const int begin = max(0, k0 - t0) & ~31;
+    const int last = min(k0 + KTILE, a.N) - 1;
+    int end = (int)min((int64_t)a.q, (int64_t)last - t0 + a.W);
+    const int2* lo_of = left.lo ? left.lo + (int64_t)(skv * a.G / a.heads) * ((a.q + 31) / 32) : nullptr;
+    if (lo_of) {                                             // ... that belong to the same sequence
+        int most = -1;
+        for (int i = begin / 32 + tid; i < (end + 31) / 32; i += NT)
+            if (lo_of[i].x <= last) most = i;
+        most = wave_max_i(most);
+        if (lane == 0) range[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = max(most, range[w]);
+        end = min(end, 32 * (__builtin_amdgcn_readfirstlane(most) + 1));
+    }
+    f32x16_t ak[MT], av[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) ak[mt] = av[mt] = f32x16_t{};
+
+    // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys
+    auto rows32 = [&](const unsigned char* qt, const unsigned char* gt, const float* sz, const float* sd, const int* sl, int row0, int r,
+                      auto edge) {
+        f32x16_t S = f32x16_t{}, dP;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(sd + row0 + result_row(i) + 4 * h);
+            dP[i] = x.x; dP[i + 1] = x.y; dP[i + 2] = x.z; dP[i + 3] = x.w;
+        }
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) {
+            Opnd<T> x;
+            QG::rows(x, qt, row0, e, h, m32);
+            S = mma(x, k[e], S);
+            QG::rows(x, gt, row0, e, h, m32);
+            dP = mma(x, v[e], dP);
+        }
+        float p[16], ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(sz + row0 + result_row(i) + 4 * h);
+            const float z[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                p[i + e] = fast_exp2(fmaf(S[i + e], c2, z[e]));
+                ds[i + e] = p[i + e] * dP[i + e];
+                if constexpr (decltype(edge)::value) {
+                    const int o = result_row(i + e) + 4 * h;
+                    const bool on = r + o < a.q && key <= t0 + r + o && key >= sl[row0 + o];
+                    p[i + e] = on ? p[i + e] : 0.f;
+                    ds[i + e] = on ? ds[i + e] : 0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            Opnd<T> pp, pd;
+            pack_opnd(pp, p + 8 * j);
+            pack_opnd(pd, ds + 8 * j);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                Opnd<T> x;
+                QG::cols(x, gt, row0 + 16 * j, mt, lane);
+                av[mt] = mma(x, pp, av[mt]);
+                QG::cols(x, qt, row0 + 16 * j, mt, lane);
+                ak[mt] = mma(x, pd, ak[mt]);
+            }
+        }
+    };
+    const int per = begin < end ? (end - begin + QT - 1) / QT : 0, total = per * a.G;    // tiles of a head, of all
+    typename QG::template Moved<NT> mq, mg;
+    float nz = 0.f, nd = 0.f;
+    int nl = 0;
+    auto fetch = [&](int i) {
+        const int s = skv * a.G + i / per, r = begin + i % per * QT;
+        const int64_t base = (int64_t)s * a.q;
+        mq.load(Q + base * D, r, a.q - 1, tid);
+        mg.load(dO + base * D, r, a.q - 1, tid);
+        if (tid < QT) {
+            const int rr = min(r + tid, a.q - 1);
+            nz = -lse[base + rr] * kLog2e;
+            nd = -left.D[base + rr];
+            nl = window_first(a, s, rr);
+        }
+    };
+    auto put = [&](int buf) {
+        mq.store(smem + buf * 2 * QG::BYTES, tid);
+        mg.store(smem + buf * 2 * QG::BYTES + QG::BYTES, tid);
+        if (tid < QT) {
+            stat_z[buf][tid] = nz;
+            stat_d[buf][tid] = nd;
+            stat_lo[buf][tid] = nl;
+        }
+    };
+    if (total > 0) {
+        fetch(0);
+        put(0);
+        __syncthreads();
+        for (int i = 0, buf = 0; i < total; ++i, buf ^= 1) {
+            if (i + 1 < total) fetch(i + 1);
+            const unsigned char* qt = smem + buf * 2 * QG::BYTES;
+            const int r0 = begin + i % per * QT;
+#pragma unroll
+            for (int x = 0; x < QT / 32; ++x) {
+                const int r = r0 + 32 * x;
+                if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N) continue;
+                int2 lo = make_int2(max(0, t0 + r - a.W + 1), max(0, t0 + r + 31 - a.W + 1));
+                if (lo_of) lo = lo_of[r / 32];
+                if (__builtin_amdgcn_readfirstlane(lo.x) > ku + 31) continue;
+                const bool full = r + 31 < a.q && t0 + r >= ku + 31 && __builtin_amdgcn_readfirstlane(lo.y) <= ku;
+                if (full) rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, std::false_type());
+                else rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, std::true_type());
+            }
+            if (i + 1 < total) put(buf ^ 1);
+            __syncthreads();
+        }
+    }
+    bool odd = false;
+    if (key < a.N) {
+        const int64_t at = ((int64_t)skv * a.rows + key) * D;
+        auto store = [&](T* to, const float (&o)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[e]) < INFINITY);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+            else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+        };
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int64_t o = at + 32 * mt + result_row(i) + 4 * h;
+                const float x[4] = {ak[mt][i] * a.scale, ak[mt][i + 1] * a.scale, ak[mt][i + 2] * a.scale, ak[mt][i + 3] * a.scale};
+                const float y[4] = {av[mt][i], av[mt][i + 1], av[mt][i + 2], av[mt][i + 3]};
+                store(dK + o, x);
+                store(dV + o, y);
+            }
+    }
+    // keys with a sum that is not finite once more, from their own pairs alone
+    uint64_t bad = __ballot(odd);
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    for (; bad; bad &= bad - 1) plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, left.D, dK, dV, skv, ku + __builtin_ctzll(bad), lane);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
-                                                          const T* __restrict__ V, const T* __restrict__ dO,
-                                                          const float* __restrict__ lse, const float* __restrict__ Dv,
-                                                          T* __restrict__ dK, T* __restrict__ dV)
-{
-    const int u = blockIdx.x * 4 + threadIdx.x / kWave;
-    if (u < a.N) plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, Dv, dK, dV, blockIdx.y, u, threadIdx.x % kWave);
-}
+// [D of every row][first keys of 32 rows each]
+static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
+size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
-size_t window_backward_ws_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
-
-template <typename T, int D>
+template <typename T, int D, int NW, int KT, int QT>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                              const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,
                              void* ws, hipStream_t st)
 {
     const WindowArgs a = window_args(s, first);
-    float* Dv = static_cast<float*>(ws);
-    const int64_t rows = (int64_t)s.bh * s.q, per = 256 / (D / 8);
-    hipLaunchKernelGGL((window_rowdot_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st,
-                       (const T*)O, (const T*)dO, Dv, rows);
-    hipError_t e = hipGetLastError();
+    const WindowLeft left = {static_cast<float*>(ws), first ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr};
+    constexpr size_t lds_q = 4 * Tile<T, D, KT>::BYTES, lds_k = 4 * Tile<T, D, QT>::BYTES;
+    auto* dq = window_dq_kernel<T, D, NW, KT>;
+    auto* dkdv = window_dkdv_kernel<T, D, NW, QT>;
+    hipError_t e = ensure_dynamic_lds((const void*)dq, lds_q);
+    if (e == hipSuccess) e = ensure_dynamic_lds((const void*)dkdv, lds_k);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_dq_kernel<T, D>), dim3((s.q + 3) / 4, s.bh), dim3(256), 0, st, a, (const T*)Q, (const T*)K,
-                       (const T*)V, (const T*)dO, lse, Dv, (T*)dQ);
+    const int qtiles = (s.q + 32 * NW - 1) / (32 * NW), ktiles = (s.N + 32 * NW - 1) / (32 * NW);
+    hipLaunchKernelGGL(dq, dim3((unsigned)schedule_grid(s.bhk, s.G * qtiles)), dim3(NW * kWave), lds_q, st, a, (const T*)Q,
+                       (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO, (T*)dQ, left, qtiles);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((window_dkdv_kernel<T, D>), dim3((s.N + 3) / 4, s.bhk), dim3(256), 0, st, a, (const T*)Q,
-                       (const T*)K, (const T*)V, (const T*)dO, lse, Dv, (T*)dK, (T*)dV);
+    hipLaunchKernelGGL(dkdv, dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(NW * kWave), lds_k, st, a, (const T*)Q,
+                       (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV, left, ktiles);
     return hipGetLastError();
 }
 
@@ -69,10 +358,10 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
                                   void* ws, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? backward_t<bf16_t, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                         : backward_t<bf16_t, 128>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                     : backward_t<float, 128>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                         : backward_t<bf16_t, 128, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<float, 64, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                     : backward_t<float, 128, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 
 }  // namespace moba
