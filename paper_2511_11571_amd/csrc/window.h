@@ -165,6 +165,11 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
 size_t window_forward_ws_bytes(const WindowDims& s);
 hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                                  void* O, float* lse, void* ws, hipStream_t st);
+// few tiles of queries (window_few.hip)
+bool window_few(const WindowDims& s);
+size_t window_few_ws_bytes(const WindowDims& s);
+hipError_t launch_window_few(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
+                             void* O, float* lse, void* ws, hipStream_t st);
 size_t window_backward_ws_bytes(const WindowDims& s);
 hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                                   const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,

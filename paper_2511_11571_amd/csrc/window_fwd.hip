@@ -180,7 +180,7 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
     }
 }
 
-size_t window_forward_ws_bytes(const WindowDims&) { return 0; }
+size_t window_forward_ws_bytes(const WindowDims& s) { return window_few(s) ? window_few_ws_bytes(s) : 0; }
 
 template <typename T, int D, int CT, int NW, int KT>
 static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
@@ -200,8 +200,9 @@ static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, con
 }
 
 hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
-                                 void* O, float* lse, void*, hipStream_t st)
+                                 void* O, float* lse, void* ws, hipStream_t st)
 {
+    if (window_few(s)) return launch_window_few(s, Q, K, V, first, O, lse, ws, st);
     if (s.dtype == MOBA_BF16)
         return s.D == 64 ? tiles_t<bf16_t, 64, 1, 4, 64>(s, Q, K, V, first, O, lse, st)
                          : tiles_t<bf16_t, 128, 1, 4, 64>(s, Q, K, V, first, O, lse, st);
