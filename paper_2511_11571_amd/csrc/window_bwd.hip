@@ -17,8 +17,8 @@ struct WindowLeft {
     int2* lo;                   // [batch][ceil(q / 32)]; rows that attend nothing count as INT_MAX in the smallest
 };
 
-template <typename T, int D, int NW, int KT>
-__global__ __launch_bounds__(NW* kWave) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+template <typename T, int D, int NW, int KT, int OCC>
+__global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                               const T* __restrict__ V, const T* __restrict__ O,
                                                               const float* __restrict__ lse, const T* __restrict__ dO,
                                                               T* __restrict__ dQ, WindowLeft left, int ntiles)
@@ -104,18 +104,18 @@ __global__ __launch_bounds__(NW* kWave) void window_dq_kernel(WindowArgs a, cons
             }
     };
     if (begin < end) {
-        typename KV::template Moved<NT> mk, mv;
-        mk.load(Ks, begin, a.N - 1, tid);
-        mv.load(Vs, begin, a.N - 1, tid);
-        mk.store(smem, tid);
-        mv.store(smem + KV::BYTES, tid);
+        u32x4_t mk[KV::template pieces<NT>], mv[KV::template pieces<NT>];
+        KV::template load<NT>(mk, Ks, begin, a.N - 1, tid);
+        KV::template load<NT>(mv, Vs, begin, a.N - 1, tid);
+        KV::template store<NT>(mk, smem, tid);
+        KV::template store<NT>(mv, smem + KV::BYTES, tid);
         __syncthreads();
         int buf = 0;
         for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
             const bool more = u0 + KT < end;
             if (more) {
-                mk.load(Ks, u0 + KT, a.N - 1, tid);
-                mv.load(Vs, u0 + KT, a.N - 1, tid);
+                KV::template load<NT>(mk, Ks, u0 + KT, a.N - 1, tid);
+                KV::template load<NT>(mv, Vs, u0 + KT, a.N - 1, tid);
             }
             const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(NW* kWave) void window_dq_kernel(WindowArgs a, cons
             }
             if (more) {
                 unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
-                mk.store(to, tid);
-                mv.store(to + KV::BYTES, tid);
+                KV::template store<NT>(mk, to, tid);
+                KV::template store<NT>(mv, to + KV::BYTES, tid);
             }
             __syncthreads();
         }
@@ -156,8 +156,8 @@ __global__ __launch_bounds__(NW* kWave) void window_dq_kernel(WindowArgs a, cons
     for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, left.D, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
 
-template <typename T, int D, int NW, int QT>
-__global__ __launch_bounds__(NW* kWave) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+template <typename T, int D, int NW, int QT, int OCC>
+__global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                                 const T* __restrict__ V, const float* __restrict__ lse,
                                                                 const T* __restrict__ dO, T* __restrict__ dK,
                                                                 T* __restrict__ dV, WindowLeft left, int ntiles)
@@ -253,14 +253,14 @@ __global__ __launch_bounds__(NW* kWave) void window_dkdv_kernel(WindowArgs a, co
         }
     };
     const int per = begin < end ? (end - begin + QT - 1) / QT : 0, total = per * a.G;    // tiles of a head, of all
-    typename QG::template Moved<NT> mq, mg;
+    u32x4_t mq[QG::template pieces<NT>], mg[QG::template pieces<NT>];
     float nz = 0.f, nd = 0.f;
     int nl = 0;
     auto fetch = [&](int i) {
         const int s = skv * a.G + i / per, r = begin + i % per * QT;
         const int64_t base = (int64_t)s * a.q;
-        mq.load(Q + base * D, r, a.q - 1, tid);
-        mg.load(dO + base * D, r, a.q - 1, tid);
+        QG::template load<NT>(mq, Q + base * D, r, a.q - 1, tid);
+        QG::template load<NT>(mg, dO + base * D, r, a.q - 1, tid);
         if (tid < QT) {
             const int rr = min(r + tid, a.q - 1);
             nz = -lse[base + rr] * kLog2e;
@@ -269,8 +269,8 @@ __global__ __launch_bounds__(NW* kWave) void window_dkdv_kernel(WindowArgs a, co
         }
     };
     auto put = [&](int buf) {
-        mq.store(smem + buf * 2 * QG::BYTES, tid);
-        mg.store(smem + buf * 2 * QG::BYTES + QG::BYTES, tid);
+        QG::template store<NT>(mq, smem + buf * 2 * QG::BYTES, tid);
+        QG::template store<NT>(mg, smem + buf * 2 * QG::BYTES + QG::BYTES, tid);
         if (tid < QT) {
             stat_z[buf][tid] = nz;
             stat_d[buf][tid] = nd;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(NW* kWave) void window_dkdv_kernel(WindowArgs a, co
 static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
 size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
-template <typename T, int D, int NW, int KT, int QT>
+template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                              const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,
                              void* ws, hipStream_t st)
@@ -338,8 +338,8 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     const WindowArgs a = window_args(s, first);
     const WindowLeft left = {static_cast<float*>(ws), first ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr};
     constexpr size_t lds_q = 4 * Tile<T, D, KT>::BYTES, lds_k = 4 * Tile<T, D, QT>::BYTES;
-    auto* dq = window_dq_kernel<T, D, NW, KT>;
-    auto* dkdv = window_dkdv_kernel<T, D, NW, QT>;
+    auto* dq = window_dq_kernel<T, D, NW, KT, OCCQ>;
+    auto* dkdv = window_dkdv_kernel<T, D, NW, QT, OCCK>;
     hipError_t e = ensure_dynamic_lds((const void*)dq, lds_q);
     if (e == hipSuccess) e = ensure_dynamic_lds((const void*)dkdv, lds_k);
     if (e != hipSuccess) return e;
@@ -358,10 +358,10 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
                                   void* ws, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                         : backward_t<bf16_t, 128, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                     : backward_t<float, 128, 4, 32, 32>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                     : backward_t<float, 128, 4, 32, 32, 1, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 
 }  // namespace moba

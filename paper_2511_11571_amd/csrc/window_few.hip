@@ -20,7 +20,7 @@ template <int D>
 constexpr int kPartWords = D + 2;
 
 template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves* kWave) void window_few_kernel(WindowArgs a, const T* __restrict__ Q,
+__global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void window_few_kernel(WindowArgs a, const T* __restrict__ Q,
                                                                       const T* __restrict__ K, const T* __restrict__ V,
                                                                       T* __restrict__ O, float* __restrict__ lse,
                                                                       float* __restrict__ part, int groups, int shares, int each)
@@ -102,19 +102,19 @@ __global__ __launch_bounds__(kFewWaves* kWave) void window_few_kernel(WindowArgs
             }
     };
     {
-        typename KV::template Moved<kWave> mk, mv;
+        u32x4_t mk[KV::template pieces<kWave>], mv[KV::template pieces<kWave>];
         int u = first + wave * kFewKeys;
         if (u < end) {
-            mk.load(Ks, u, a.N - 1, lane);
-            mv.load(Vs, u, a.N - 1, lane);
+            KV::template load<kWave>(mk, Ks, u, a.N - 1, lane);
+            KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
         }
         for (; u < end; u += NW * kFewKeys) {
             // (the wave's own LDS: its reads of the keys before are done before these stores, in order)
-            mk.store(mine, lane);
-            mv.store(mine + KV::BYTES, lane);
+            KV::template store<kWave>(mk, mine, lane);
+            KV::template store<kWave>(mv, mine + KV::BYTES, lane);
             if (u + NW * kFewKeys < end) {
-                mk.load(Ks, u + NW * kFewKeys, a.N - 1, lane);
-                mv.load(Vs, u + NW * kFewKeys, a.N - 1, lane);
+                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
+                KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
             }
             if (u + kFewKeys - 1 <= t_min && u >= lo_max && u + kFewKeys <= end) keys32(u, std::false_type());
             else keys32(u, std::true_type());

@@ -119,18 +119,18 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
             }
     };
     if (begin < end) {
-        typename KV::template Moved<NT> mk, mv;
-        mk.load(Ks, begin, a.N - 1, tid);
-        mv.load(Vs, begin, a.N - 1, tid);
-        mk.store(smem, tid);
-        mv.store(smem + KV::BYTES, tid);
+        u32x4_t mk[KV::template pieces<NT>], mv[KV::template pieces<NT>];
+        KV::template load<NT>(mk, Ks, begin, a.N - 1, tid);
+        KV::template load<NT>(mv, Vs, begin, a.N - 1, tid);
+        KV::template store<NT>(mk, smem, tid);
+        KV::template store<NT>(mv, smem + KV::BYTES, tid);
         __syncthreads();
         int buf = 0;
         for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
             const bool more = u0 + KT < end;
             if (more) {
-                mk.load(Ks, u0 + KT, a.N - 1, tid);
-                mv.load(Vs, u0 + KT, a.N - 1, tid);
+                KV::template load<NT>(mk, Ks, u0 + KT, a.N - 1, tid);
+                KV::template load<NT>(mv, Vs, u0 + KT, a.N - 1, tid);
             }
             const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
@@ -142,8 +142,8 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
             }
             if (more) {
                 unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
-                mk.store(to, tid);
-                mv.store(to + KV::BYTES, tid);
+                KV::template store<NT>(mk, to, tid);
+                KV::template store<NT>(mv, to + KV::BYTES, tid);
             }
             __syncthreads();
         }

@@ -46,30 +46,28 @@ template <typename T, int D, int ROWS>
 struct Tile {
     static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, BYTES = ROWS * RB;
 
-    // what a workgroup of NT threads moves from memory to LDS: PER pieces of every thread
+    // what NT threads move from memory to LDS: `pieces` of every thread
     template <int NT>
-    struct Moved {
-        static constexpr int PER = ROWS * PIECES / NT;
-        static_assert(ROWS * PIECES % NT == 0, "whole pieces");
-        uint4 x[PER];
-        // rows first .. first + ROWS of a slice, rows from last + 1 on replaced by row `last`
-        __device__ __forceinline__ void load(const T* __restrict__ slice, int first, int last, int tid)
-        {
+    static constexpr int pieces = ROWS * PIECES / NT;
+    // rows first .. first + ROWS of a slice, rows from last + 1 on replaced by row `last`
+    template <int NT>
+    static __device__ __forceinline__ void load(u32x4_t (&x)[ROWS * PIECES / NT], const T* __restrict__ slice, int first, int last, int tid)
+    {
+        static_assert(ROWS * PIECES % NT == 0 && (NT % PIECES == 0), "whole pieces");
+        const int row = first + tid / PIECES;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int id = tid + i * NT, row = min(first + id / PIECES, last);
-                x[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(slice) + (int64_t)row * RB + 16 * (id % PIECES));
-            }
-        }
-        __device__ __forceinline__ void store(unsigned char* tile, int tid) const
-        {
+        for (int i = 0; i < ROWS * PIECES / NT; ++i)
+            x[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(slice) + (int64_t)min(row + i * (NT / PIECES), last) * RB + 16 * (tid % PIECES));
+    }
+    template <int NT>
+    static __device__ __forceinline__ void store(const u32x4_t (&x)[ROWS * PIECES / NT], unsigned char* tile, int tid)
+    {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int id = tid + i * NT, row = id / PIECES;
-                *reinterpret_cast<uint4*>(tile + row * RB + 16 * ((id % PIECES) ^ (row & 7))) = x[i];
-            }
+        for (int i = 0; i < ROWS * PIECES / NT; ++i) {
+            const int row = tid / PIECES + i * (NT / PIECES);
+            *reinterpret_cast<u32x4_t*>(tile + row * RB + 16 * ((tid % PIECES) ^ (row & 7))) = x[i];
         }
-    };
+    }
 
     // rows row0 + m, channels 16 c + 8 h .. + 7 (row0 a multiple of 8)
     static __device__ __forceinline__ void rows(Opnd<T>& o, const unsigned char* tile, int row0, int c, int h, int m)
