@@ -70,7 +70,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     f32x16_t acc[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, auto edge) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool edge) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -Dr;
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
-            if constexpr (decltype(edge)::value) {
+            if (edge) {
                 const int key = u + result_row(i) + 4 * h;
                 x[i] = key <= t && key >= lo ? x[i] : 0.f;
             }
@@ -122,8 +122,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
                 if (u > t_max || u + 31 < lo_min) continue;
-                if (u + 31 <= t_min && u >= lo_max) keys32(kt, kt + KV::BYTES, 32 * x, u, std::false_type());
-                else keys32(kt, kt + KV::BYTES, 32 * x, u, std::true_type());
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
             }
             if (more) {
                 unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
@@ -205,7 +204,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 
     // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys
     auto rows32 = [&](const unsigned char* qt, const unsigned char* gt, const float* sz, const float* sd, const int* sl, int row0, int r,
-                      auto edge) {
+                      bool edge) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
@@ -229,7 +228,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             for (int e = 0; e < 4; ++e) {
                 p[i + e] = fast_exp2(fmaf(S[i + e], c2, z[e]));
                 ds[i + e] = p[i + e] * dP[i + e];
-                if constexpr (decltype(edge)::value) {
+                if (edge) {
                     const int o = result_row(i + e) + 4 * h;
                     const bool on = r + o < a.q && key <= t0 + r + o && key >= sl[row0 + o];
                     p[i + e] = on ? p[i + e] : 0.f;
@@ -293,8 +292,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
                 if (lo_of) lo = lo_of[r / 32];
                 if (__builtin_amdgcn_readfirstlane(lo.x) > ku + 31) continue;
                 const bool full = r + 31 < a.q && t0 + r >= ku + 31 && __builtin_amdgcn_readfirstlane(lo.y) <= ku;
-                if (full) rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, std::false_type());
-                else rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, std::true_type());
+                rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, !full);
             }
             if (i + 1 < total) put(buf ^ 1);
             __syncthreads();
@@ -358,9 +356,9 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
                                   void* ws, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
                      : backward_t<float, 128, 4, 32, 32, 1, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 

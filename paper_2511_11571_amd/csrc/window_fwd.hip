@@ -12,8 +12,8 @@
 
 namespace moba {
 
-template <typename T, int D, int CT, int NW, int KT>
-__global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
+template <typename T, int D, int CT, int NW, int KT, int OCC>
+__global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
                                                                    const T* __restrict__ K, const T* __restrict__ V,
                                                                    T* __restrict__ O, float* __restrict__ lse, int ntiles)
 {
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[c][mt] = f32x16_t{};
     }
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, auto edge) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool edge) {
         f32x16_t S[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) S[c] = f32x16_t{};
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 x[i] = S[c][i];
-                if constexpr (decltype(edge)::value) {
+                if (edge) {
                     const int key = u + result_row(i) + 4 * h;
                     x[i] = key <= t[c] && key >= lo[c] ? x[i] : -INFINITY;
                 }
@@ -137,8 +137,7 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
                 if (u > t_max || u + 31 < lo_min) continue;
-                if (u + 31 <= t_min && u >= lo_max) keys32(kt, kt + KV::BYTES, 32 * x, u, std::false_type());
-                else keys32(kt, kt + KV::BYTES, 32 * x, u, std::true_type());
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
             }
             if (more) {
                 unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
@@ -182,11 +181,11 @@ __global__ __launch_bounds__(NW* kWave) void window_forward_kernel(WindowArgs a,
 
 size_t window_forward_ws_bytes(const WindowDims& s) { return window_few(s) ? window_few_ws_bytes(s) : 0; }
 
-template <typename T, int D, int CT, int NW, int KT>
+template <typename T, int D, int CT, int NW, int KT, int OCC>
 static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                           void* O, float* lse, hipStream_t st)
 {
-    auto* kernel = window_forward_kernel<T, D, CT, NW, KT>;
+    auto* kernel = window_forward_kernel<T, D, CT, NW, KT, OCC>;
     constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
     if (lds > 64 * 1024) {
         const hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
@@ -204,10 +203,10 @@ hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void*
 {
     if (window_few(s)) return launch_window_few(s, Q, K, V, first, O, lse, ws, st);
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? tiles_t<bf16_t, 64, 1, 4, 64>(s, Q, K, V, first, O, lse, st)
-                         : tiles_t<bf16_t, 128, 1, 4, 64>(s, Q, K, V, first, O, lse, st);
-    return s.D == 64 ? tiles_t<float, 64, 1, 4, 32>(s, Q, K, V, first, O, lse, st)
-                     : tiles_t<float, 128, 1, 4, 32>(s, Q, K, V, first, O, lse, st);
+        return s.D == 64 ? tiles_t<bf16_t, 64, 1, 4, 64, 4>(s, Q, K, V, first, O, lse, st)
+                         : tiles_t<bf16_t, 128, 1, 4, 64, 2>(s, Q, K, V, first, O, lse, st);
+    return s.D == 64 ? tiles_t<float, 64, 1, 4, 32, 3>(s, Q, K, V, first, O, lse, st)
+                     : tiles_t<float, 128, 1, 4, 32, 2>(s, Q, K, V, first, O, lse, st);
 }
 
 }  // namespace moba
