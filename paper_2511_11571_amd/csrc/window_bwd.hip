@@ -84,9 +84,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
         }
         float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
-            if (edge) {
+        for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
                 const int key = u + result_row(i) + 4 * h;
                 x[i] = key <= t && key >= lo ? x[i] : 0.f;
             }
@@ -228,12 +229,15 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             for (int e = 0; e < 4; ++e) {
                 p[i + e] = fast_exp2(fmaf(S[i + e], c2, z[e]));
                 ds[i + e] = p[i + e] * dP[i + e];
-                if (edge) {
-                    const int o = result_row(i + e) + 4 * h;
-                    const bool on = r + o < a.q && key <= t0 + r + o && key >= sl[row0 + o];
-                    p[i + e] = on ? p[i + e] : 0.f;
-                    ds[i + e] = on ? ds[i + e] : 0.f;
-                }
+            }
+        }
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int o = result_row(i) + 4 * h;
+                const bool on = r + o < a.q && key <= t0 + r + o && key >= sl[row0 + o];
+                p[i] = on ? p[i] : 0.f;
+                ds[i] = on ? ds[i] : 0.f;
             }
         }
 #pragma unroll

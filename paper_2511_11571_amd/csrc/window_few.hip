@@ -66,14 +66,16 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
         }
         float x[16], top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = S[i];
-            if (edge) {
+        for (int i = 0; i < 16; ++i) x[i] = S[i];
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
                 const int key = u + result_row(i) + 4 * h;
                 x[i] = key <= t && key >= lo ? x[i] : -INFINITY;
             }
-            top = max_nan(top, x[i]);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max_nan(top, x[i]);
         top = max_halves(top) * c2;
         if (__ballot(top > ref + 8.f)) {
             const float now = fmaxf(ref, top), alpha = fast_exp2(ref - now);
@@ -82,13 +84,9 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[mt] *= alpha;
         }
-        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = fast_exp2(fmaf(x[i], c2, -ref));
-            sum += x[i];
-        }
-        l += sum;
+        for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref));
+        l += sum16(x);
         Opnd<T> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
@@ -189,28 +187,28 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     }
 }
 
-// A wave per row: its parts, in their order
+// A workgroup per row: its waves take the row's parts in turn, eight on their way at a time, and are added up in order
 template <typename T, int D>
-__global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
-                                                           const T* __restrict__ V, T* __restrict__ O, float* __restrict__ lse,
-                                                           const float* __restrict__ part, int groups, int shares)
+__global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+                                                                        const T* __restrict__ V, T* __restrict__ O, float* __restrict__ lse,
+                                                                        const float* __restrict__ part, int groups, int shares)
 {
+    __shared__ float wave_sum[kFewWaves][D + 2];
     const int lane = threadIdx.x % kWave, rows = a.G * a.q;
-    const int64_t i = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (i >= (int64_t)a.bhk * rows) return;
-    const int skv = (int)(i / rows), idx = (int)(i % rows), r = idx / a.G, s = skv * a.G + idx % a.G;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int skv = blockIdx.x / rows, idx = blockIdx.x % rows, r = idx / a.G, s = skv * a.G + idx % a.G;
     const float* p = part + (((int64_t)skv * groups + idx / 32) * shares * 32 + idx % 32) * kPartWords<D>;
     const int64_t step = 32 * kPartWords<D>;
     float top = kLowest;
     for (int x = lane; x < shares; x += kWave) top = fmaxf(top, p[x * step]);
     top = wave_max(top);
     float L = 0.f, o[D / 64] = {};
-    constexpr int U = 8;                                     // parts in flight
-    for (int x0 = 0; x0 < shares; x0 += U) {
+    constexpr int U = 8;
+    for (int x0 = wave; x0 < shares; x0 += U * kFewWaves) {
         float m[U], l[U], y[U][D / 64];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float* at = p + min(x0 + u, shares - 1) * step;
+            const float* at = p + min(x0 + u * kFewWaves, shares - 1) * step;
             m[u] = at[0];
             l[u] = at[1];
 #pragma unroll
@@ -218,12 +216,22 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, const T
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (x0 + u >= shares) break;
+            if (x0 + u * kFewWaves >= shares) break;
             const float w = fast_exp2(m[u] - top);
             L = fmaf(w, l[u], L);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) o[c] = fmaf(w, y[u][c], o[c]);
         }
+    }
+    if (lane == 0) wave_sum[wave][0] = L;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) wave_sum[wave][2 + lane + 64 * c] = o[c];
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < kFewWaves; ++w) {
+        L += wave_sum[w][0];
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] += wave_sum[w][2 + lane + 64 * c];
     }
     const bool empty = window_first(a, s, r) > a.N - a.q + r;
     const int64_t row = (int64_t)s * a.q + r;
@@ -275,8 +283,7 @@ static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const
                        (const T*)Q, (const T*)K, (const T*)V, (T*)O, lse, (float*)ws, groups, shares, each);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares == 1) return e;
-    const int64_t rows = (int64_t)s.bh * s.q;
-    hipLaunchKernelGGL((window_merge_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, (const T*)Q,
+    hipLaunchKernelGGL((window_merge_kernel<T, D>), dim3((unsigned)(s.bh * s.q)), dim3(kFewWaves * kWave), 0, st, a, (const T*)Q,
                        (const T*)K, (const T*)V, (T*)O, lse, (const float*)ws, groups, shares);
     return hipGetLastError();
 }

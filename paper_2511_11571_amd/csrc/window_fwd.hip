@@ -80,9 +80,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
         for (int c = 0; c < CT; ++c) {
             float x[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = S[c][i];
-                if (edge) {
+            for (int i = 0; i < 16; ++i) x[i] = S[c][i];
+            if (edge) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
                     const int key = u + result_row(i) + 4 * h;
                     x[i] = key <= t[c] && key >= lo[c] ? x[i] : -INFINITY;
                 }
@@ -98,13 +99,9 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) acc[c][mt] *= alpha;
             }
-            float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = fast_exp2(fmaf(x[i], c2, -ref[c]));
-                sum += x[i];
-            }
-            l[c] += sum;
+            for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref[c]));
+            l[c] += sum16(x);
             pack_opnd(p[c][0], x);
             pack_opnd(p[c][1], x + 8);
         }

@@ -41,6 +41,15 @@ __device__ __forceinline__ void pack_opnd(Opnd<float>& o, const float* p)
     for (int e = 0; e < 8; ++e) o.v[e] = p[e];
 }
 
+// sum of sixteen probabilities as they are before they are rounded (in pairs: short chains)
+__device__ __forceinline__ float sum16(const float (&x)[16])
+{
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (x[i] + x[4 + i]) + (x[8 + i] + x[12 + i]);
+    return (y[0] + y[1]) + (y[2] + y[3]);
+}
+
 // A tile of ROWS rows of D channels in LDS
 template <typename T, int D, int ROWS>
 struct Tile {
