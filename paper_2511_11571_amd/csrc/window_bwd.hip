@@ -105,19 +105,13 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             }
     };
     if (begin < end) {
-        u32x4_t mk[KV::template pieces<NT>], mv[KV::template pieces<NT>];
-        KV::template load<NT>(mk, Ks, begin, a.N - 1, tid);
-        KV::template load<NT>(mv, Vs, begin, a.N - 1, tid);
-        KV::template store<NT>(mk, smem, tid);
-        KV::template store<NT>(mv, smem + KV::BYTES, tid);
+        Coming<KV, T, NT, false> next;
+        next.start(smem, Ks, Vs, begin, a.N - 1, tid);
+        next.finish(smem, tid);
         __syncthreads();
-        int buf = 0;
-        for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
-            const bool more = u0 + KT < end;
-            if (more) {
-                KV::template load<NT>(mk, Ks, u0 + KT, a.N - 1, tid);
-                KV::template load<NT>(mv, Vs, u0 + KT, a.N - 1, tid);
-            }
+        for (int u0 = begin, buf = 0; u0 < end; u0 += KT, buf ^= 1) {
+            unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
             const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
@@ -125,11 +119,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
                 if (u > t_max || u + 31 < lo_min) continue;
                 keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
             }
-            if (more) {
-                unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
-                KV::template store<NT>(mk, to, tid);
-                KV::template store<NT>(mv, to + KV::BYTES, tid);
-            }
+            if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
         }
     }
@@ -156,7 +146,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, left.D, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
 
-template <typename T, int D, int NW, int QT, int OCC>
+template <typename T, int D, int NW, int QT, int OCC, bool DIRECT>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                                 const T* __restrict__ V, const float* __restrict__ lse,
                                                                 const T* __restrict__ dO, T* __restrict__ dK,
@@ -167,7 +157,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     using QG = Tile<T, D, QT>;
     extern __shared__ __align__(16) unsigned char smem[];    // Q, dO | Q, dO
     __shared__ __align__(16) float stat_z[2][QT], stat_d[2][QT];             // -lse (log2 units), -D
-    __shared__ int stat_lo[2][QT], range[NW];
+    __shared__ __align__(16) int stat_lo[2][QT];
+    __shared__ int range[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int skv, tile;
@@ -232,12 +223,18 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             }
         }
         if (edge) {
+            const int late = min(a.q, key - t0) - r, past = a.q - r;      // rows of the tile from `late` on see the key, as far as they exist
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int o = result_row(i) + 4 * h;
-                const bool on = r + o < a.q && key <= t0 + r + o && key >= sl[row0 + o];
-                p[i] = on ? p[i] : 0.f;
-                ds[i] = on ? ds[i] : 0.f;
+            for (int i = 0; i < 16; i += 4) {
+                const int4 x = *reinterpret_cast<const int4*>(sl + row0 + result_row(i) + 4 * h);
+                const int lo[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int o = result_row(i + e) + 4 * h;
+                    const bool on = (o >= late) & (o < past) & (key >= lo[e]);
+                    p[i + e] = on ? p[i + e] : 0.f;
+                    ds[i + e] = on ? ds[i + e] : 0.f;
+                }
             }
         }
 #pragma unroll
@@ -256,50 +253,54 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
         }
     };
     const int per = begin < end ? (end - begin + QT - 1) / QT : 0, total = per * a.G;    // tiles of a head, of all
-    u32x4_t mq[QG::template pieces<NT>], mg[QG::template pieces<NT>];
     float nz = 0.f, nd = 0.f;
     int nl = 0;
-    auto fetch = [&](int i) {
+    Coming<QG, T, NT, DIRECT> next;
+    int2 lo_next[QT / 32], lo_here[QT / 32];
+    auto fetch = [&](int i, int buf) {
         const int s = skv * a.G + i / per, r = begin + i % per * QT;
         const int64_t base = (int64_t)s * a.q;
-        QG::template load<NT>(mq, Q + base * D, r, a.q - 1, tid);
-        QG::template load<NT>(mg, dO + base * D, r, a.q - 1, tid);
         if (tid < QT) {
             const int rr = min(r + tid, a.q - 1);
             nz = -lse[base + rr] * kLog2e;
             nd = -left.D[base + rr];
             nl = window_first(a, s, rr);
         }
+#pragma unroll
+        for (int x = 0; x < QT / 32; ++x) {
+            const int rx = min(r + 32 * x, a.q - 1);
+            lo_next[x] = lo_of ? lo_of[rx / 32] : make_int2(max(0, t0 + rx - a.W + 1), max(0, t0 + rx + 31 - a.W + 1));
+        }
+        next.start(smem + buf * 2 * QG::BYTES, Q + base * D, dO + base * D, r, a.q - 1, tid);
     };
-    auto put = [&](int buf) {
-        QG::template store<NT>(mq, smem + buf * 2 * QG::BYTES, tid);
-        QG::template store<NT>(mg, smem + buf * 2 * QG::BYTES + QG::BYTES, tid);
+    // the tile is there: its rows' statistics go to LDS, too
+    auto arrived = [&](int buf) {
+        next.finish(smem + buf * 2 * QG::BYTES, tid);
         if (tid < QT) {
             stat_z[buf][tid] = nz;
             stat_d[buf][tid] = nd;
             stat_lo[buf][tid] = nl;
         }
+#pragma unroll
+        for (int x = 0; x < QT / 32; ++x)
+            lo_here[x] = make_int2(__builtin_amdgcn_readfirstlane(lo_next[x].x), __builtin_amdgcn_readfirstlane(lo_next[x].y));
+        __syncthreads();
     };
     if (total > 0) {
-        fetch(0);
-        put(0);
-        __syncthreads();
+        fetch(0, 0);
+        arrived(0);
         for (int i = 0, buf = 0; i < total; ++i, buf ^= 1) {
-            if (i + 1 < total) fetch(i + 1);
+            if (i + 1 < total) fetch(i + 1, buf ^ 1);
             const unsigned char* qt = smem + buf * 2 * QG::BYTES;
             const int r0 = begin + i % per * QT;
 #pragma unroll
             for (int x = 0; x < QT / 32; ++x) {
                 const int r = r0 + 32 * x;
-                if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N) continue;
-                int2 lo = make_int2(max(0, t0 + r - a.W + 1), max(0, t0 + r + 31 - a.W + 1));
-                if (lo_of) lo = lo_of[r / 32];
-                if (__builtin_amdgcn_readfirstlane(lo.x) > ku + 31) continue;
-                const bool full = r + 31 < a.q && t0 + r >= ku + 31 && __builtin_amdgcn_readfirstlane(lo.y) <= ku;
+                if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N || lo_here[x].x > ku + 31) continue;
+                const bool full = r + 31 < a.q && t0 + r >= ku + 31 && lo_here[x].y <= ku;
                 rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, !full);
             }
-            if (i + 1 < total) put(buf ^ 1);
-            __syncthreads();
+            if (i + 1 < total) arrived(buf ^ 1);
         }
     }
     bool odd = false;
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
 size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
-template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK>
+template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                              const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,
                              void* ws, hipStream_t st)
@@ -341,7 +342,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     const WindowLeft left = {static_cast<float*>(ws), first ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr};
     constexpr size_t lds_q = 4 * Tile<T, D, KT>::BYTES, lds_k = 4 * Tile<T, D, QT>::BYTES;
     auto* dq = window_dq_kernel<T, D, NW, KT, OCCQ>;
-    auto* dkdv = window_dkdv_kernel<T, D, NW, QT, OCCK>;
+    auto* dkdv = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT>;
     hipError_t e = ensure_dynamic_lds((const void*)dq, lds_q);
     if (e == hipSuccess) e = ensure_dynamic_lds((const void*)dkdv, lds_k);
     if (e != hipSuccess) return e;
@@ -360,10 +361,10 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
                                   void* ws, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                     : backward_t<float, 128, 4, 32, 32, 1, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2, false>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 2, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                     : backward_t<float, 128, 4, 32, 32, 1, 1, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 
 }  // namespace moba

@@ -116,19 +116,13 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
             }
     };
     if (begin < end) {
-        u32x4_t mk[KV::template pieces<NT>], mv[KV::template pieces<NT>];
-        KV::template load<NT>(mk, Ks, begin, a.N - 1, tid);
-        KV::template load<NT>(mv, Vs, begin, a.N - 1, tid);
-        KV::template store<NT>(mk, smem, tid);
-        KV::template store<NT>(mv, smem + KV::BYTES, tid);
+        Coming<KV, T, NT, false> next;
+        next.start(smem, Ks, Vs, begin, a.N - 1, tid);
+        next.finish(smem, tid);
         __syncthreads();
-        int buf = 0;
-        for (int u0 = begin; u0 < end; u0 += KT, buf ^= 1) {
-            const bool more = u0 + KT < end;
-            if (more) {
-                KV::template load<NT>(mk, Ks, u0 + KT, a.N - 1, tid);
-                KV::template load<NT>(mv, Vs, u0 + KT, a.N - 1, tid);
-            }
+        for (int u0 = begin, buf = 0; u0 < end; u0 += KT, buf ^= 1) {
+            unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
             const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
@@ -136,11 +130,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
                 if (u > t_max || u + 31 < lo_min) continue;
                 keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
             }
-            if (more) {
-                unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
-                KV::template store<NT>(mk, to, tid);
-                KV::template store<NT>(mv, to + KV::BYTES, tid);
-            }
+            if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
         }
     }

@@ -78,6 +78,24 @@ struct Tile {
         }
     }
 
+    // The same straight into LDS: a wave's instruction fills 1 KB, so a lane fetches the piece that belongs at its place.
+    // The caller waits (fetched()) before the barrier after which the tile is read.
+    template <int NT>
+    static __device__ __forceinline__ void fetch(unsigned char* tile, const T* __restrict__ slice, int first, int last, int tid)
+    {
+        static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0 && NT / PIECES % 8 == 0, "whole pieces, the same exchange in all");
+        const int row = tid / PIECES, piece = (tid % PIECES) ^ (row & 7);
+        const char* from = reinterpret_cast<const char*>(slice) + 16 * piece;
+        const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+#pragma unroll
+        for (int i = 0; i < ROWS * PIECES / NT; ++i) {
+            const char* at = from + (int64_t)min(first + row + i * (NT / PIECES), last) * RB;
+const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
+            // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory", "m0");
+        }
+    }
+
     // rows row0 + m, channels 16 c + 8 h .. + 7 (row0 a multiple of 8)
     static __device__ __forceinline__ void rows(Opnd<T>& o, const unsigned char* tile, int row0, int c, int h, int m)
     {
@@ -108,6 +126,38 @@ struct Tile {
                 const int r = 8 * (s >> 2) + 4 * h + (s & 3);
                 o.v[s] = *reinterpret_cast<const float*>(tile + (row0 + r) * RB + 128 * mt + 16 * ((m >> 2) ^ (r & 7)) + 4 * (m & 3));
             }
+        }
+    }
+};
+
+__device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Two tiles, one behind the other in LDS, on their way while a workgroup of NT threads works on two others: through
+// registers, or (DIRECT) straight into LDS, which takes fewer registers but costs time where there are enough: d = 64,
+// 2 x 16 heads of 8192, dense, us through registers -> direct: dQ 424 -> 451, dK and dV 603 -> 648; d = 128, 16 heads
+// on 4 of 32768, W = 2048: forward 622 -> 636, dQ 845 -> 880, dK and dV 1793 -> 1305 (24 registers spilled -> 10).
+template <class TILE, typename T, int NT, bool DIRECT>
+struct Coming {
+    static constexpr int P = DIRECT ? 1 : TILE::template pieces<NT>;
+    u32x4_t x[P], y[P];
+    __device__ __forceinline__ void start(unsigned char* to, const T* __restrict__ a, const T* __restrict__ b, int first, int last, int tid)
+    {
+        if constexpr (DIRECT) {
+            TILE::template fetch<NT>(to, a, first, last, tid);
+            TILE::template fetch<NT>(to + TILE::BYTES, b, first, last, tid);
+        } else {
+            TILE::template load<NT>(x, a, first, last, tid);
+            TILE::template load<NT>(y, b, first, last, tid);
+        }
+    }
+    // (a barrier has to follow)
+    __device__ __forceinline__ void finish(unsigned char* to, int tid)
+    {
+        if constexpr (DIRECT) {
+            fetched();
+        } else {
+            TILE::template store<NT>(x, to, tid);
+            TILE::template store<NT>(y, to + TILE::BYTES, tid);
         }
     }
 };
