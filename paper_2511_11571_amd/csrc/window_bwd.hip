@@ -70,7 +70,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     f32x16_t acc[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool edge) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -Dr;
@@ -85,12 +85,13 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
-        if (edge) {
+        if (late) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = u + result_row(i) + 4 * h;
-                x[i] = key <= t && key >= lo ? x[i] : 0.f;
-            }
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= t - u - 4 * h ? x[i] : 0.f;
+        }
+        if (early) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : 0.f;
         }
         Opnd<T> p[2];
         pack_opnd(p[0], x);
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
                 if (u > t_max || u + 31 < lo_min) continue;
-                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min, u < lo_max);
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 
     // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys
     auto rows32 = [&](const unsigned char* qt, const unsigned char* gt, const float* sz, const float* sd, const int* sl, int row0, int r,
-                      bool edge) {
+                      bool late, bool early) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
@@ -222,18 +223,29 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
                 ds[i + e] = p[i + e] * dP[i + e];
             }
         }
-        if (edge) {
-            const int late = min(a.q, key - t0) - r, past = a.q - r;      // rows of the tile from `late` on see the key, as far as they exist
+        // rows from the key's own on ...
+        auto only = [&](int i, bool on) {
+            p[i] = on ? p[i] : 0.f;
+            ds[i] = on ? ds[i] : 0.f;
+        };
+        if (late) {
+            const int least = key - t0 - r - 4 * h;
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int4 x = *reinterpret_cast<const int4*>(sl + row0 + result_row(i) + 4 * h);
-                const int lo[4] = {x.x, x.y, x.z, x.w};
+            for (int i = 0; i < 16; ++i) only(i, result_row(i) >= least);
+        }
+        if (early) {
+            // ... up to the last that exists and whose window still holds it; with first keys, by each row's own
+            const int most = min(a.q - 1 - r, key - t0 - r + a.W - 1) - 4 * h;               // (sums of numbers up to 2^24)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int o = result_row(i + e) + 4 * h;
-                    const bool on = (o >= late) & (o < past) & (key >= lo[e]);
-                    p[i + e] = on ? p[i + e] : 0.f;
-                    ds[i + e] = on ? ds[i + e] : 0.f;
+            for (int i = 0; i < 16; ++i) only(i, result_row(i) <= most);
+            if (lo_of) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(sl + row0 + result_row(i) + 4 * h);
+                    only(i, key >= x.x);
+                    only(i + 1, key >= x.y);
+                    only(i + 2, key >= x.z);
+                    only(i + 3, key >= x.w);
                 }
             }
         }
@@ -297,8 +309,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             for (int x = 0; x < QT / 32; ++x) {
                 const int r = r0 + 32 * x;
                 if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N || lo_here[x].x > ku + 31) continue;
-                const bool full = r + 31 < a.q && t0 + r >= ku + 31 && lo_here[x].y <= ku;
-                rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, !full);
+                rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, t0 + r < ku + 31, r + 31 >= a.q || lo_here[x].y > ku);
             }
             if (i + 1 < total) arrived(buf ^ 1);
         }

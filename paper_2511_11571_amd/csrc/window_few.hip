@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
     float ref = kLowest, l = 0.f;
-    auto keys32 = [&](int u, bool edge) {
+    auto keys32 = [&](int u, bool late, bool early) {
         f32x16_t S = f32x16_t{};
 #pragma unroll
         for (int e = 0; e < STEPS; ++e) {
@@ -67,12 +67,13 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
         float x[16], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = S[i];
-        if (edge) {
+        if (late) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int key = u + result_row(i) + 4 * h;
-                x[i] = key <= t && key >= lo ? x[i] : -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= t - u - 4 * h ? x[i] : -INFINITY;
+        }
+        if (early) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : -INFINITY;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = max_nan(top, x[i]);
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
                 KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
                 KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
             }
-            keys32(u, u + kFewKeys - 1 > t_min || u < lo_max);
+            keys32(u, u + kFewKeys - 1 > t_min, u < lo_max);
         }
     }
     // ---- merge the waves: O of every wave to LDS, 16-byte pieces of row m exchanged by m & 7

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[c][mt] = f32x16_t{};
     }
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool edge) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) {
         f32x16_t S[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) S[c] = f32x16_t{};
@@ -81,12 +81,15 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
             float x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = S[c][i];
-            if (edge) {
+            if (late) {
+                const int most = t[c] - u - 4 * h;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = u + result_row(i) + 4 * h;
-                    x[i] = key <= t[c] && key >= lo[c] ? x[i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= most ? x[i] : -INFINITY;
+            }
+            if (early) {
+                const int least = lo[c] - u - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= least ? x[i] : -INFINITY;
             }
             float top = x[0];
 #pragma unroll
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
                 if (u > t_max || u + 31 < lo_min) continue;
-                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min || u < lo_max);
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min, u < lo_max);
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();

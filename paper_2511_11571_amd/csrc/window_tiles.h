@@ -6,8 +6,9 @@
 // 8 j .. 8 j + 7 of a result are therefore the second operand of step j of a product over its rows, whose slot
 // 8 h + s is row 16 j + 8 (s >> 2) + 4 h + (s & 3): probabilities never change lanes.
 //
-// Tiles of rows lie in LDS row by row, the 16-byte pieces of row r at places exchanged by r & 7: rows read as
-// operands (a piece of 32 rows at once) and columns (four rows by sixteen channels at once) both use all banks.
+// Tiles of rows lie in LDS row by row, the 16-byte pieces of a row at places exchanged by place(row): sixteen rows
+// read at one piece (operands of rows) and four rows at four neighbouring pieces (columns) both cover the 64
+// banks, 256 bytes, once.  Exchanged by row & 7, both met banks two and four times: d = 128, W = 2048, a third of the time.
 #pragma once
 #include "window.h"
 
@@ -54,6 +55,10 @@ __device__ __forceinline__ float sum16(const float (&x)[16])
 template <typename T, int D, int ROWS>
 struct Tile {
     static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, BYTES = ROWS * RB;
+    static __device__ __forceinline__ constexpr int place(int row)
+    {
+        return PIECES == 8 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3);
+    }
 
     // what NT threads move from memory to LDS: `pieces` of every thread
     template <int NT>
@@ -74,7 +79,7 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < ROWS * PIECES / NT; ++i) {
             const int row = tid / PIECES + i * (NT / PIECES);
-            *reinterpret_cast<u32x4_t*>(tile + row * RB + 16 * ((tid % PIECES) ^ (row & 7))) = x[i];
+            *reinterpret_cast<u32x4_t*>(tile + row * RB + 16 * ((tid % PIECES) ^ place(row))) = x[i];
         }
     }
 
@@ -83,48 +88,48 @@ struct Tile {
     template <int NT>
     static __device__ __forceinline__ void fetch(unsigned char* tile, const T* __restrict__ slice, int first, int last, int tid)
     {
-        static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0 && NT / PIECES % 8 == 0, "whole pieces, the same exchange in all");
-        const int row = tid / PIECES, piece = (tid % PIECES) ^ (row & 7);
-        const char* from = reinterpret_cast<const char*>(slice) + 16 * piece;
+        static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0, "whole pieces");
         const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
 #pragma unroll
         for (int i = 0; i < ROWS * PIECES / NT; ++i) {
-            const char* at = from + (int64_t)min(first + row + i * (NT / PIECES), last) * RB;
-const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
+            const int row = tid / PIECES + i * (NT / PIECES);
+            const char* at = reinterpret_cast<const char*>(slice) + (int64_t)min(first + row, last) * RB + 16 * ((tid % PIECES) ^ place(row));
+            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
             // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory", "m0");
         }
     }
 
-    // rows row0 + m, channels 16 c + 8 h .. + 7 (row0 a multiple of 8)
+    // rows row0 + m, channels 16 c + 8 h .. + 7 (row0 a multiple of 16)
     static __device__ __forceinline__ void rows(Opnd<T>& o, const unsigned char* tile, int row0, int c, int h, int m)
     {
         const unsigned char* p = tile + (row0 + m) * RB;
         if constexpr (sizeof(T) == 2) {
-            o.f.q = *reinterpret_cast<const uint4*>(p + (16 * ((2 * c) ^ (h ^ (m & 7)))));
+            o.f.q = *reinterpret_cast<const uint4*>(p + ((32 * c) ^ (16 * (h ^ place(m)))));
         } else {
-            const float4 a = *reinterpret_cast<const float4*>(p + 16 * ((4 * c) ^ ((2 * h) ^ (m & 7))));
-            const float4 b = *reinterpret_cast<const float4*>(p + 16 * ((4 * c) ^ ((2 * h + 1) ^ (m & 7))));
+            const float4 a = *reinterpret_cast<const float4*>(p + ((64 * c) ^ (16 * ((2 * h) ^ place(m)))));
+            const float4 b = *reinterpret_cast<const float4*>(p + ((64 * c) ^ (16 * ((2 * h + 1) ^ place(m)))));
             o.v[0] = a.x; o.v[1] = a.y; o.v[2] = a.z; o.v[3] = a.w;
             o.v[4] = b.x; o.v[5] = b.y; o.v[6] = b.z; o.v[7] = b.w;
         }
     }
     // the transpose: channel 32 mt + m, slots in the order of a result's rows, of rows row0 .. row0 + 15
-    // (row0 a multiple of 8)
+    // (row0 a multiple of 16; rows eight apart have places that differ by 2)
     static __device__ __forceinline__ void cols(Opnd<T>& o, const unsigned char* tile, int row0, int mt, int lane)
     {
         const int h = lane >> 5;
         if constexpr (sizeof(T) == 2) {
-            const int e = (lane & 15) >> 2, q = lane & 3;
-            const unsigned char* p = tile + (row0 + 4 * h + e) * RB + ((64 * mt) ^ (16 * ((2 * ((lane >> 4) & 1) + (q >> 1)) ^ (4 * h + e)))) + 8 * (q & 1);
-            const uint2 a = lds_read_tr16(p), b = lds_read_tr16(p + 8 * RB);
+            const int row = 4 * h + ((lane & 15) >> 2), q = lane & 3;
+            const int at = (64 * mt) ^ (16 * ((2 * ((lane >> 4) & 1) + (q >> 1)) ^ place(row)));
+            const unsigned char* p = tile + (row0 + row) * RB + 8 * (q & 1);
+            const uint2 a = lds_read_tr16(p + at), b = lds_read_tr16(p + 8 * RB + (at ^ 32));
             o.f.u[0] = a.x; o.f.u[1] = a.y; o.f.u[2] = b.x; o.f.u[3] = b.y;
         } else {
             const int m = lane & 31;
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const int r = 8 * (s >> 2) + 4 * h + (s & 3);
-                o.v[s] = *reinterpret_cast<const float*>(tile + (row0 + r) * RB + 128 * mt + 16 * ((m >> 2) ^ (r & 7)) + 4 * (m & 3));
+                o.v[s] = *reinterpret_cast<const float*>(tile + (row0 + r) * RB + ((128 * mt) ^ (16 * ((m >> 2) ^ place(r)))) + 4 * (m & 3));
             }
         }
     }
