@@ -70,7 +70,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     f32x16_t acc[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -Dr;
@@ -110,10 +110,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
         next.start(smem, Ks, Vs, begin, a.N - 1, tid);
         next.finish(smem, tid);
         __syncthreads();
-        for (int u0 = begin, buf = 0; u0 < end; u0 += KT, buf ^= 1) {
-            unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+        // (the two buffers by turns, each with its own code: places in LDS are constants)
+        auto step = [&](int u0, auto buf) __attribute__((always_inline)) {
+            const unsigned char* kt = smem + decltype(buf)::value * 2 * KV::BYTES;
+            unsigned char* to = smem + (decltype(buf)::value ^ 1) * 2 * KV::BYTES;
             if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
-            const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
@@ -122,6 +123,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
+        };
+        for (int u0 = begin; u0 < end; u0 += 2 * KT) {
+            step(u0, std::integral_constant<int, 0>());
+            if (u0 + KT < end) step(u0 + KT, std::integral_constant<int, 1>());
         }
     }
     bool odd = false;
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 
     // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys
     auto rows32 = [&](const unsigned char* qt, const unsigned char* gt, const float* sz, const float* sd, const int* sl, int row0, int r,
-                      bool late, bool early) {
+                      bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             }
         }
         // rows from the key's own on ...
-        auto only = [&](int i, bool on) {
+        auto only = [&](int i, bool on) __attribute__((always_inline)) {
             p[i] = on ? p[i] : 0.f;
             ds[i] = on ? ds[i] : 0.f;
         };
@@ -264,13 +269,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             }
         }
     };
-    const int per = begin < end ? (end - begin + QT - 1) / QT : 0, total = per * a.G;    // tiles of a head, of all
     float nz = 0.f, nd = 0.f;
     int nl = 0;
     Coming<QG, T, NT, DIRECT> next;
     int2 lo_next[QT / 32], lo_here[QT / 32];
-    auto fetch = [&](int i, int buf) {
-        const int s = skv * a.G + i / per, r = begin + i % per * QT;
+    auto fetch = [&](int g, int r, int buf) __attribute__((always_inline)) {
+        const int s = skv * a.G + g;
         const int64_t base = (int64_t)s * a.q;
         if (tid < QT) {
             const int rr = min(r + tid, a.q - 1);
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
         next.start(smem + buf * 2 * QG::BYTES, Q + base * D, dO + base * D, r, a.q - 1, tid);
     };
     // the tile is there: its rows' statistics go to LDS, too
-    auto arrived = [&](int buf) {
+    auto arrived = [&](int buf) __attribute__((always_inline)) {
         next.finish(smem + buf * 2 * QG::BYTES, tid);
         if (tid < QT) {
             stat_z[buf][tid] = nz;
@@ -298,20 +302,24 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             lo_here[x] = make_int2(__builtin_amdgcn_readfirstlane(lo_next[x].x), __builtin_amdgcn_readfirstlane(lo_next[x].y));
         __syncthreads();
     };
-    if (total > 0) {
-        fetch(0, 0);
+    if (begin < end) {
+        fetch(0, begin, 0);
         arrived(0);
-        for (int i = 0, buf = 0; i < total; ++i, buf ^= 1) {
-            if (i + 1 < total) fetch(i + 1, buf ^ 1);
+        int g = 0, r0 = begin, buf = 0;
+        for (bool more = true; more; buf ^= 1) {
+            const int r_here = r0;
+            r0 += QT;
+            if (r0 >= end) { r0 = begin; ++g; }
+            more = g < a.G;
+            if (more) fetch(g, r0, buf ^ 1);
             const unsigned char* qt = smem + buf * 2 * QG::BYTES;
-            const int r0 = begin + i % per * QT;
 #pragma unroll
             for (int x = 0; x < QT / 32; ++x) {
-                const int r = r0 + 32 * x;
+                const int r = r_here + 32 * x;
                 if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N || lo_here[x].x > ku + 31) continue;
                 rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, t0 + r < ku + 31, r + 31 >= a.q || lo_here[x].y > ku);
             }
-            if (i + 1 < total) arrived(buf ^ 1);
+            if (more) arrived(buf ^ 1);
         }
     }
     bool odd = false;

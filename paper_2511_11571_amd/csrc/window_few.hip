@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
     float ref = kLowest, l = 0.f;
-    auto keys32 = [&](int u, bool late, bool early) {
+    auto keys32 = [&](int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{};
 #pragma unroll
         for (int e = 0; e < STEPS; ++e) {

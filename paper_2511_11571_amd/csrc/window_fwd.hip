@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[c][mt] = f32x16_t{};
     }
-    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) {
+    auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) S[c] = f32x16_t{};
@@ -123,10 +123,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
         next.start(smem, Ks, Vs, begin, a.N - 1, tid);
         next.finish(smem, tid);
         __syncthreads();
-        for (int u0 = begin, buf = 0; u0 < end; u0 += KT, buf ^= 1) {
-            unsigned char* to = smem + (buf ^ 1) * 2 * KV::BYTES;
+        // (the two buffers by turns, each with its own code: places in LDS are constants)
+        auto step = [&](int u0, auto buf) __attribute__((always_inline)) {
+            const unsigned char* kt = smem + decltype(buf)::value * 2 * KV::BYTES;
+            unsigned char* to = smem + (decltype(buf)::value ^ 1) * 2 * KV::BYTES;
             if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
-            const unsigned char* kt = smem + buf * 2 * KV::BYTES;
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
@@ -135,6 +136,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
+        };
+        for (int u0 = begin; u0 < end; u0 += 2 * KT) {
+            step(u0, std::integral_constant<int, 0>());
+            if (u0 + KT < end) step(u0 + KT, std::integral_constant<int, 1>());
         }
     }
     if (r0 >= a.q) return;

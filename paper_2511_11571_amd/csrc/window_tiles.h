@@ -68,10 +68,18 @@ struct Tile {
     static __device__ __forceinline__ void load(u32x4_t (&x)[ROWS * PIECES / NT], const T* __restrict__ slice, int first, int last, int tid)
     {
         static_assert(ROWS * PIECES % NT == 0 && (NT % PIECES == 0), "whole pieces");
-        const int row = first + tid / PIECES;
+        constexpr int STEP = NT / PIECES;
+        if (first + ROWS - 1 <= last) {                      // (one offset for all lanes' pieces, the rest is scalar)
+            const char* from = reinterpret_cast<const char*>(slice) + (int64_t)first * RB;
+            const uint32_t at = 16u * (uint32_t)tid;
 #pragma unroll
-        for (int i = 0; i < ROWS * PIECES / NT; ++i)
-            x[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(slice) + (int64_t)min(row + i * (NT / PIECES), last) * RB + 16 * (tid % PIECES));
+            for (int i = 0; i < ROWS * PIECES / NT; ++i) x[i] = *reinterpret_cast<const u32x4_t*>(from + i * (STEP * RB) + at);
+        } else {
+            const int row = first + tid / PIECES;
+#pragma unroll
+            for (int i = 0; i < ROWS * PIECES / NT; ++i)
+                x[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(slice) + (int64_t)min(row + i * STEP, last) * RB + 16 * (tid % PIECES));
+        }
     }
     template <int NT>
     static __device__ __forceinline__ void store(const u32x4_t (&x)[ROWS * PIECES / NT], unsigned char* tile, int tid)
