@@ -170,6 +170,12 @@ bool window_few(const WindowDims& s);
 size_t window_few_ws_bytes(const WindowDims& s);
 hipError_t launch_window_few(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                              void* O, float* lse, void* ws, hipStream_t st);
+bool window_few_dq(const WindowDims& s);
+bool window_few_dkdv(const WindowDims& s);
+hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
+                                const void* dO, const int32_t* first, void* dQ, float* Dv, hipStream_t st);
+hipError_t launch_window_few_dkdv(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
+                                  const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st);
 size_t window_backward_ws_bytes(const WindowDims& s);
 hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                                   const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,

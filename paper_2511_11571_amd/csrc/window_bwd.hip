@@ -11,17 +11,33 @@
 
 namespace moba {
 
-// what the dQ kernel leaves: D of every row and, with first keys, the smallest and largest of 32 rows each
+// what the kernel for dK and dV finds: D of every row and, with first keys, the smallest and largest of 32 rows each
 struct WindowLeft {
-    float* D;                   // [bh][q]
-    int2* lo;                   // [batch][ceil(q / 32)]; rows that attend nothing count as INT_MAX in the smallest
+    const float* D;             // [bh][q]
+    const int2* lo;             // [batch][ceil(q / 32)]; rows that attend nothing count as INT_MAX in the smallest
 };
+
+// those, where the kernel for dQ by tiles has not left them: a wave per two lots of 32 rows
+__global__ __launch_bounds__(256) void window_lo_kernel(WindowArgs a, int2* __restrict__ lo, int lots)
+{
+    const int i = blockIdx.x * 8 + threadIdx.x / 32, b = blockIdx.y;
+    const int r = min(i * 32 + (int)threadIdx.x % 32, a.q - 1);
+    const int first = window_first(a, b * a.heads, r);
+    int least = first <= a.N - a.q + r ? first : 0x7fffffff, most = first;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        least = min(least, __shfl_xor(least, o, 32));
+        most = max(most, __shfl_xor(most, o, 32));
+    }
+    if (i < lots && threadIdx.x % 32 == 0) lo[(int64_t)b * lots + i] = make_int2(least, most);
+}
 
 template <typename T, int D, int NW, int KT, int OCC>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                               const T* __restrict__ V, const T* __restrict__ O,
                                                               const float* __restrict__ lse, const T* __restrict__ dO,
-                                                              T* __restrict__ dQ, WindowLeft left, int ntiles)
+                                                              T* __restrict__ dQ, float* __restrict__ Dv,
+                                                              int2* __restrict__ lo_out, int ntiles)
 {
     constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
     using KV = Tile<T, D, KT>;
@@ -52,13 +68,13 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     }
     Dr = sum_halves(Dr);
     const bool mine = r0 + m32 < a.q;
-    if (mine && h == 0) left.D[row] = Dr;
+    if (mine && h == 0) Dv[row] = Dr;
     const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
     const int lo_min = r0 < a.q ? wave_min_i(lo <= t ? lo : 0x7fffffff) : 0x7fffffff, lo_max = wave_max_i(lo);
     const int t_min = t0 + min(r0, a.q - 1), t_max = t0 + min(r0 + 31, a.q - 1);
     if (lane == 0) {
         wg_lo[wave] = lo_min;
-        if (left.lo && s % a.heads == 0 && r0 < a.q) left.lo[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(lo_min, lo_max);
+        if (lo_out && s % a.heads == 0 && r0 < a.q) lo_out[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(lo_min, lo_max);
     }
     __syncthreads();
     int begin = wg_lo[0];
@@ -149,7 +165,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     // rows with a sum that is not finite once more, from their own pairs alone
     uint64_t bad = __ballot(odd);
     bad = (bad | bad >> 32) & 0xffffffffu;
-    for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, left.D, dQ, s, r0 + __builtin_ctzll(bad), lane);
+    for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, Dv, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
 
 template <typename T, int D, int NW, int QT, int OCC, bool DIRECT>
@@ -358,20 +374,38 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
                              void* ws, hipStream_t st)
 {
     const WindowArgs a = window_args(s, first);
-    const WindowLeft left = {static_cast<float*>(ws), first ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr};
-    constexpr size_t lds_q = 4 * Tile<T, D, KT>::BYTES, lds_k = 4 * Tile<T, D, QT>::BYTES;
-    auto* dq = window_dq_kernel<T, D, NW, KT, OCCQ>;
-    auto* dkdv = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT>;
-    hipError_t e = ensure_dynamic_lds((const void*)dq, lds_q);
-    if (e == hipSuccess) e = ensure_dynamic_lds((const void*)dkdv, lds_k);
+    float* Dv = static_cast<float*>(ws);
+    const bool few_q = window_few_dq(s), few_k = window_few_dkdv(s);
+    int2* lo = first && !few_k ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr;
+    hipError_t e;
+    if (few_q) {
+        e = launch_window_few_dq(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);
+        if (e != hipSuccess) return e;
+    } else {
+        constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
+        auto* kernel = window_dq_kernel<T, D, NW, KT, OCCQ>;
+        e = ensure_dynamic_lds((const void*)kernel, lds);
+        if (e != hipSuccess) return e;
+        const int tiles = (s.q + 32 * NW - 1) / (32 * NW);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, s.G * tiles)), dim3(NW * kWave), lds, st, a, (const T*)Q,
+                           (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO, (T*)dQ, Dv, lo, tiles);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (few_k) return launch_window_few_dkdv(s, Q, K, V, lse, dO, first, dK, dV, Dv, st);
+    if (lo && few_q) {
+        const int lots = (s.q + 31) / 32;
+        hipLaunchKernelGGL(window_lo_kernel, dim3((lots + 7) / 8, s.batch), dim3(256), 0, st, a, lo, lots);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    constexpr size_t lds = 4 * Tile<T, D, QT>::BYTES;
+    auto* kernel = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT>;
+    e = ensure_dynamic_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
-    const int qtiles = (s.q + 32 * NW - 1) / (32 * NW), ktiles = (s.N + 32 * NW - 1) / (32 * NW);
-    hipLaunchKernelGGL(dq, dim3((unsigned)schedule_grid(s.bhk, s.G * qtiles)), dim3(NW * kWave), lds_q, st, a, (const T*)Q,
-                       (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO, (T*)dQ, left, qtiles);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(dkdv, dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(NW * kWave), lds_k, st, a, (const T*)Q,
-                       (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV, left, ktiles);
+    const int tiles = (s.N + 32 * NW - 1) / (32 * NW);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, tiles)), dim3(NW * kWave), lds, st, a, (const T*)Q, (const T*)K,
+                       (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV, WindowLeft{Dv, lo}, tiles);
     return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
-// Causal attention to the last W keys: forward where there are few tiles of queries -- the tokens of a serving
-// step against a cache, short calls.
+// Causal attention to the last W keys where there are few tiles of queries -- the tokens of a serving step against
+// a cache, short calls -- forward and backward.
 //
 // The G q_len queries of a key/value head count as one sequence of rows, position by position, 32 of which are the
 // columns of every product: keys and values are read once for all heads that share them.  The waves of a workgroup
@@ -18,6 +18,41 @@ constexpr int kFewKeys = 32;            // keys a wave takes at a time
 // parts of rows shared by workgroups: [slice][32 rows each][share][row][m (log2 units), l, O]
 template <int D>
 constexpr int kPartWords = D + 2;
+
+// O of 32 rows of every wave through LDS, 16-byte pieces of row m exchanged by m & 7; then every thread takes CH
+// channels ch0 .. of row c
+template <int D>
+struct WaveSums {
+    static constexpr int NW = kFewWaves, TPR = NW * kWave / 32, CH = D / TPR;
+    static __device__ __forceinline__ void put(unsigned char* mine, const f32x16_t (&acc)[D / 32], int h, int m32)
+    {
+#pragma unroll
+        for (int mt = 0; mt < D / 32; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int piece = (32 * mt + result_row(i) + 4 * h) / 4;
+                *reinterpret_cast<float4*>(mine + m32 * D * 4 + 16 * (piece ^ (m32 & 7))) =
+                    make_float4(acc[mt][i], acc[mt][i + 1], acc[mt][i + 2], acc[mt][i + 3]);
+            }
+    }
+    // o += w_wave * what the waves put
+    template <typename F>
+    static __device__ __forceinline__ void add(float (&o)[CH], const unsigned char* smem, int wave_bytes, int c, int ch0, F weight)
+    {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float wt = weight(w);
+#pragma unroll
+            for (int e = 0; e < CH; e += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(smem + w * wave_bytes + c * D * 4 + 16 * (((ch0 + e) / 4) ^ (c & 7)));
+                o[e] = fmaf(wt, x.x, o[e]);
+                o[e + 1] = fmaf(wt, x.y, o[e + 1]);
+                o[e + 2] = fmaf(wt, x.z, o[e + 2]);
+                o[e + 3] = fmaf(wt, x.w, o[e + 3]);
+            }
+        }
+    }
+};
 
 template <typename T, int D>
 __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void window_few_kernel(WindowArgs a, const T* __restrict__ Q,
@@ -118,19 +153,13 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             keys32(u, u + kFewKeys - 1 > t_min, u < lo_max);
         }
     }
-    // ---- merge the waves: O of every wave to LDS, 16-byte pieces of row m exchanged by m & 7
+    // ---- merge the waves
     l = sum_halves(l);
     if (h == 0) { wave_ref[wave][m32] = ref; wave_l[wave][m32] = l; }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int piece = (32 * mt + result_row(i) + 4 * h) / 4;
-            *reinterpret_cast<float4*>(mine + m32 * D * 4 + 16 * (piece ^ (m32 & 7))) =
-                make_float4(acc[mt][i], acc[mt][i + 1], acc[mt][i + 2], acc[mt][i + 3]);
-        }
+    using Sums = WaveSums<D>;
+    constexpr int TPR = Sums::TPR, CH = Sums::CH;
+    Sums::put(mine, acc, h, m32);
     __syncthreads();
-    constexpr int TPR = NW * kWave / 32, CH = D / TPR;       // threads of a row, channels of a thread
     const int c = tid / TPR, ch0 = tid % TPR * CH;
     float top = kLowest, L = 0.f, o[CH];
 #pragma unroll
@@ -138,18 +167,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, wave_ref[w][c]);
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const float wt = fast_exp2(wave_ref[w][c] - top);
-        L = fmaf(wt, wave_l[w][c], L);
-#pragma unroll
-        for (int e = 0; e < CH; e += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(smem + w * WAVE_BYTES + c * D * 4 + 16 * (((ch0 + e) / 4) ^ (c & 7)));
-            o[e] = fmaf(wt, x.x, o[e]);
-            o[e + 1] = fmaf(wt, x.y, o[e + 1]);
-            o[e + 2] = fmaf(wt, x.z, o[e + 2]);
-            o[e + 3] = fmaf(wt, x.w, o[e + 3]);
-        }
-    }
+    for (int w = 0; w < NW; ++w) L = fmaf(fast_exp2(wave_ref[w][c] - top), wave_l[w][c], L);
+    Sums::add(o, smem, WAVE_BYTES, c, ch0, [&](int w) { return fast_exp2(wave_ref[w][c] - top); });
     const int cidx = 32 * group + c;
     if (shares > 1) {
         if (cidx < rows) {
@@ -188,7 +207,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     }
 }
 
-// A workgroup per row: its waves take the row's parts in turn, eight on their way at a time, and are added up in order
+// A workgroup per row: its waves take the row's parts in turn, sixteen on their way at a time, and are added up in order
 template <typename T, int D>
 __global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                                         const T* __restrict__ V, T* __restrict__ O, float* __restrict__ lse,
@@ -200,21 +219,25 @@ __global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowAr
     const int skv = blockIdx.x / rows, idx = blockIdx.x % rows, r = idx / a.G, s = skv * a.G + idx % a.G;
     const float* p = part + (((int64_t)skv * groups + idx / 32) * shares * 32 + idx % 32) * kPartWords<D>;
     const int64_t step = 32 * kPartWords<D>;
-    float top = kLowest;
-    for (int x = lane; x < shares; x += kWave) top = fmaxf(top, p[x * step]);
-    top = wave_max(top);
-    float L = 0.f, o[D / 64] = {};
-    constexpr int U = 8;
+    float top = kLowest, L = 0.f, o[D / 64] = {};
+    constexpr int U = 16;
     for (int x0 = wave; x0 < shares; x0 += U * kFewWaves) {
-        float m[U], l[U], y[U][D / 64];
+        float m[U], l[U], y[U][D / 64], now = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < U; ++u) {                        // (past the end: the last one again, weight 0)
             const float* at = p + min(x0 + u * kFewWaves, shares - 1) * step;
             m[u] = at[0];
             l[u] = at[1];
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) y[u][c] = at[2 + lane + 64 * c];
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) now = fmaxf(now, m[u]);
+        const float alpha = fast_exp2(top - now);
+        top = now;
+        L *= alpha;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] *= alpha;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (x0 + u * kFewWaves >= shares) break;
@@ -224,15 +247,22 @@ __global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowAr
             for (int c = 0; c < D / 64; ++c) o[c] = fmaf(w, y[u][c], o[c]);
         }
     }
-    if (lane == 0) wave_sum[wave][0] = L;
+    if (lane == 0) { wave_sum[wave][0] = top; wave_sum[wave][1] = L; }
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) wave_sum[wave][2 + lane + 64 * c] = o[c];
     __syncthreads();
     if (wave > 0) return;
-    for (int w = 1; w < kFewWaves; ++w) {
-        L += wave_sum[w][0];
+    L = 0.f;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) o[c] += wave_sum[w][2 + lane + 64 * c];
+    for (int c = 0; c < D / 64; ++c) o[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, wave_sum[w][0]);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+        const float wt = fast_exp2(wave_sum[w][0] - top);
+        L = fmaf(wt, wave_sum[w][1], L);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] = fmaf(wt, wave_sum[w][2 + lane + 64 * c], o[c]);
     }
     const bool empty = window_first(a, s, r) > a.N - a.q + r;
     const int64_t row = (int64_t)s * a.q + r;
@@ -247,6 +277,297 @@ __global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowAr
     if (__ballot(odd)) plain_forward_row<T, D>(a, Q, K, V, O, lse, s, r, lane);
 }
 
+// dQ: as the forward, the waves' sums added up at the end.  D of every row is left for dK and dV.
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+                                                                            const T* __restrict__ V, const T* __restrict__ O,
+                                                                            const float* __restrict__ lse, const T* __restrict__ dO,
+                                                                            T* __restrict__ dQ, float* __restrict__ Dv, int groups)
+{
+    constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
+    using KV = Tile<T, D, kFewKeys>;
+    constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    int skv, group;
+    if (!schedule(blockIdx.x, a.bhk, groups, skv, group)) return;
+    const int rows = a.G * a.q, t0 = a.N - a.q;
+    const T* Ks = K + (int64_t)skv * a.rows * D;
+    const T* Vs = V + (int64_t)skv * a.rows * D;
+    const int idx = min(32 * group + m32, rows - 1);
+    const int r = idx / a.G, s = skv * a.G + idx % a.G, t = t0 + r, lo = window_first(a, s, r);
+    const int64_t row = (int64_t)s * a.q + r;
+    Opnd<T> q[STEPS], g[STEPS];
+    float Dr = 0.f;
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+        const int64_t at = row * D + 16 * e + 8 * h;
+        load_opnd(q[e], Q + at);
+        load_opnd(g[e], dO + at);
+        float x[8], y[8];
+        Vec8<T>::load(dO + at, x);
+        Vec8<T>::load(O + at, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) Dr = fmaf(x[i], y[i], Dr);
+    }
+    Dr = sum_halves(Dr);
+    if (wave == 0 && h == 0 && 32 * group + m32 < rows) Dv[row] = Dr;
+    const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
+    const int lo_min = wave_min_i(lo <= t ? lo : 0x7fffffff), lo_max = wave_max_i(lo);
+    const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
+    unsigned char* mine = smem + wave * WAVE_BYTES;
+    f32x16_t acc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
+    {
+        u32x4_t mk[KV::template pieces<kWave>], mv[KV::template pieces<kWave>];
+        int u = (lo_min == 0x7fffffff ? t_max + 1 : lo_min / kFewKeys * kFewKeys) + wave * kFewKeys;
+        if (u <= t_max) {
+            KV::template load<kWave>(mk, Ks, u, a.N - 1, lane);
+            KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
+        }
+        for (; u <= t_max; u += NW * kFewKeys) {
+            KV::template store<kWave>(mk, mine, lane);
+            KV::template store<kWave>(mv, mine + KV::BYTES, lane);
+            if (u + NW * kFewKeys <= t_max) {
+                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
+                KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
+            }
+            f32x16_t S = f32x16_t{}, dP;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dP[i] = -Dr;
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) {
+                Opnd<T> k, v;
+                KV::rows(k, mine, 0, e, h, m32);
+                S = mma(k, q[e], S);
+                KV::rows(v, mine + KV::BYTES, 0, e, h, m32);
+                dP = mma(v, g[e], dP);
+            }
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(S[i], c2, -z)) * dP[i];
+            if (u + kFewKeys - 1 > t_min) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= t - u - 4 * h ? x[i] : 0.f;
+            }
+            if (u < lo_max) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : 0.f;
+            }
+            Opnd<T> p[2];
+            pack_opnd(p[0], x);
+            pack_opnd(p[1], x + 8);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    Opnd<T> k;
+                    KV::cols(k, mine, 16 * j, mt, lane);
+                    acc[mt] = mma(k, p[j], acc[mt]);
+                }
+        }
+    }
+    using Sums = WaveSums<D>;
+    constexpr int TPR = Sums::TPR, CH = Sums::CH;
+    Sums::put(mine, acc, h, m32);
+    __syncthreads();
+    const int c = tid / TPR, ch0 = tid % TPR * CH;
+    float o[CH];
+#pragma unroll
+    for (int e = 0; e < CH; ++e) o[e] = 0.f;
+    Sums::add(o, smem, WAVE_BYTES, c, ch0, [](int) { return 1.f; });
+    bool odd = false;
+    int cr = 0, cs = 0;
+    if (32 * group + c < rows) {
+        cr = (32 * group + c) / a.G;
+        cs = skv * a.G + (32 * group + c) % a.G;
+        const bool empty = window_first(a, cs, cr) > t0 + cr;
+#pragma unroll
+        for (int e = 0; e < CH; e += 8) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = empty ? 0.f : o[e + i] * a.scale;
+                odd |= !(fabsf(x[i]) < INFINITY);
+            }
+            Vec8<T>::store(dQ + ((int64_t)cs * a.q + cr) * D + ch0 + e, x);
+        }
+    }
+    // rows that are not finite once more, from their own pairs alone (their D, the first wave's stores, is there since the barrier)
+    for (uint64_t bad = __ballot(odd); bad;) {
+        const int x = __builtin_ctzll(bad) / TPR;
+        bad &= ~(((1ull << TPR) - 1) << (x * TPR));
+        plain_dq_row<T, D>(a, Q, K, V, dO, lse, Dv, dQ, __shfl(cs, x * TPR, kWave), __shfl(cr, x * TPR, kWave), lane);
+    }
+}
+
+// dK and dV of 32 keys: the waves take 32 rows at a time in turn, of all heads that share the keys
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(WindowArgs a, const T* __restrict__ Q,
+                                                                              const T* __restrict__ K, const T* __restrict__ V,
+                                                                              const float* __restrict__ lse, const T* __restrict__ dO,
+                                                                              T* __restrict__ dK, T* __restrict__ dV,
+                                                                              const float* __restrict__ Dv, int ktiles)
+{
+    constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
+    using QG = Tile<T, D, 32>;
+    constexpr int WAVE_BYTES = 2 * QG::BYTES > 32 * D * 4 ? 2 * QG::BYTES : 32 * D * 4;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(16) float stat_z[NW][32], stat_d[NW][32];
+    __shared__ __align__(16) int stat_lo[NW][32];
+    __shared__ int range[NW];
+    const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    int skv, tile;
+    if (!schedule(blockIdx.x, a.bhk, ktiles, skv, tile)) return;
+    const int t0 = a.N - a.q, ku = 32 * tile, key = ku + m32;
+    Opnd<T> k[STEPS], v[STEPS];
+    const int64_t own = ((int64_t)skv * a.rows + min(key, a.N - 1)) * D;
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+        load_opnd(k[e], K + own + 16 * e + 8 * h);
+        load_opnd(v[e], V + own + 16 * e + 8 * h);
+    }
+    const float c2 = a.scale * kLog2e;
+    const int begin = max(0, ku - t0) & ~31, last = min(ku + 32, a.N) - 1;
+    int end = (int)min((int64_t)a.q, (int64_t)last - t0 + a.W);
+    if (a.first) {                                           // up to the last row that sees a key
+        int most = -1;
+        for (int r = begin + tid; r < end; r += NW * kWave)
+            if (window_first(a, skv * a.G, r) <= last) most = r;
+        most = wave_max_i(most);
+        if (lane == 0) range[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) most = max(most, range[w]);
+        end = min(end, __builtin_amdgcn_readfirstlane(most) + 1);
+    }
+    const int per = begin < end ? (end - begin + 31) / 32 : 0, total = per * a.G;
+    unsigned char* mine = smem + wave * WAVE_BYTES;
+    float *sz = stat_z[wave], *sd = stat_d[wave];
+    int* sl = stat_lo[wave];
+    f32x16_t ak[MT], av[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) ak[mt] = av[mt] = f32x16_t{};
+    {
+        u32x4_t mq[QG::template pieces<kWave>], mg[QG::template pieces<kWave>];
+        float nz = 0.f, nd = 0.f;
+        int nl = 0;
+        auto fetch = [&](int i) __attribute__((always_inline)) {
+            const int s = skv * a.G + i / per, r = begin + i % per * 32;
+            const int64_t base = (int64_t)s * a.q;
+            QG::template load<kWave>(mq, Q + base * D, r, a.q - 1, lane);
+            QG::template load<kWave>(mg, dO + base * D, r, a.q - 1, lane);
+            const int rr = min(r + m32, a.q - 1);
+            nz = -lse[base + rr] * kLog2e;
+            nd = -Dv[base + rr];
+            nl = window_first(a, s, rr);
+        };
+        if (wave < total) fetch(wave);
+        for (int i = wave; i < total; i += NW) {
+            const int r = begin + i % per * 32;
+            QG::template store<kWave>(mq, mine, lane);
+            QG::template store<kWave>(mg, mine + QG::BYTES, lane);
+            if (h == 0) { sz[m32] = nz; sd[m32] = nd; sl[m32] = nl; }
+            const bool late = t0 + r < ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;
+            if (i + NW < total) fetch(i + NW);
+            f32x16_t S = f32x16_t{}, dP;
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(sd + result_row(j) + 4 * h);
+                dP[j] = x.x; dP[j + 1] = x.y; dP[j + 2] = x.z; dP[j + 3] = x.w;
+            }
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) {
+                Opnd<T> x;
+                QG::rows(x, mine, 0, e, h, m32);
+                S = mma(x, k[e], S);
+                QG::rows(x, mine + QG::BYTES, 0, e, h, m32);
+                dP = mma(x, v[e], dP);
+            }
+            float p[16], ds[16];
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(sz + result_row(j) + 4 * h);
+                const float z[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[j + e] = fast_exp2(fmaf(S[j + e], c2, z[e]));
+                    ds[j + e] = p[j + e] * dP[j + e];
+                }
+            }
+            auto only = [&](int j, bool on) __attribute__((always_inline)) {
+                p[j] = on ? p[j] : 0.f;
+                ds[j] = on ? ds[j] : 0.f;
+            };
+            if (late) {
+                const int least = key - t0 - r - 4 * h;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) only(j, result_row(j) >= least);
+            }
+            if (early) {
+                const int most = a.q - 1 - r - 4 * h;
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(sl + result_row(j) + 4 * h);
+                    only(j, (key >= x.x) & (result_row(j) <= most));
+                    only(j + 1, (key >= x.y) & (result_row(j + 1) <= most));
+                    only(j + 2, (key >= x.z) & (result_row(j + 2) <= most));
+                    only(j + 3, (key >= x.w) & (result_row(j + 3) <= most));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                Opnd<T> pp, pd;
+                pack_opnd(pp, p + 8 * j);
+                pack_opnd(pd, ds + 8 * j);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    Opnd<T> x;
+                    QG::cols(x, mine + QG::BYTES, 16 * j, mt, lane);
+                    av[mt] = mma(x, pp, av[mt]);
+                    QG::cols(x, mine, 16 * j, mt, lane);
+                    ak[mt] = mma(x, pd, ak[mt]);
+                }
+            }
+        }
+    }
+    using Sums = WaveSums<D>;
+    constexpr int TPR = Sums::TPR, CH = Sums::CH;
+    const int c = tid / TPR, ch0 = tid % TPR * CH;
+    bool odd = false;
+    auto out = [&](const f32x16_t(&acc)[MT], T* to, float factor) __attribute__((always_inline)) {
+        Sums::put(mine, acc, h, m32);
+        __syncthreads();
+        float o[CH];
+#pragma unroll
+        for (int e = 0; e < CH; ++e) o[e] = 0.f;
+        Sums::add(o, smem, WAVE_BYTES, c, ch0, [](int) { return 1.f; });
+        if (ku + c >= a.N) return;
+#pragma unroll
+        for (int e = 0; e < CH; e += 8) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = o[e + i] * factor;
+                odd |= !(fabsf(x[i]) < INFINITY);
+            }
+            Vec8<T>::store(to + ((int64_t)skv * a.rows + ku + c) * D + ch0 + e, x);
+        }
+    };
+    out(ak, dK, a.scale);
+    __syncthreads();
+    out(av, dV, 1.f);
+    // keys that are not finite once more, from their own pairs alone
+    for (uint64_t bad = __ballot(odd); bad;) {
+        const int x = __builtin_ctzll(bad) / TPR;
+        bad &= ~(((1ull << TPR) - 1) << (x * TPR));
+        plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, Dv, dK, dV, skv, ku + __shfl(c, x * TPR, kWave), lane);
+    }
+}
+
 static int few_groups(const WindowDims& s) { return (s.G * s.q + 31) / 32; }
 // keys that 32 rows can see between them
 static int few_keys(const WindowDims& s)
@@ -254,20 +575,47 @@ static int few_keys(const WindowDims& s)
     const int64_t positions = std::min<int64_t>(s.q, (31 + s.G - 1) / s.G + 1);
     return (int)std::min<int64_t>(s.N, s.W + positions - 1);
 }
-// workgroups that share a group's keys: two for every compute unit in all, and no less than two turns of every wave
+// Workgroups that share a group's keys: one for every compute unit in all, with two turns of every wave at least; rows of
+// less than 1024 keys are not shared, for the second kernel takes 5 us.  us with at least 256 | 512 | 1024 | 2048 keys each, up to 512
+// workgroups: 1 token, 16 heads on 4, d = 128, N = 4096 10.5 | 11.8 | 14.8 | 21.4; 16384 14.2 | 13.7 | 16.0 | 22.4; 131109
+// 53.6 | 53.3 | 53.2 | 48.8 (the last is the one with 256 workgroups); unshared 31.7, 111, 844.
+constexpr int kShareKeys = 256, kSharedKeys = 1024;
 static int few_shares(const WindowDims& s)
 {
+    if (few_keys(s) < kSharedKeys) return 1;
     const int64_t items = (int64_t)s.bhk * few_groups(s);
-    const int64_t most = (few_keys(s) + 2 * kFewWaves * kFewKeys - 1) / (2 * kFewWaves * kFewKeys);
-    return (int)std::max<int64_t>(1, std::min(512 / items, most));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(256 / items, few_keys(s) / kShareKeys));
 }
-bool window_few(const WindowDims& s) { return (int64_t)s.bh * ((s.q + 127) / 128) < 256; }
+// Few tiles?  The tiled kernels take as long as their longest walk where the chip is not full, the ones here cut it in four but
+// take about 1.3 times as long where it is: few, where tiles x average walk < c x longest walk - x.  us, tiled | here, 16 heads,
+// bf16, d = 64: forward N = 1024, W = 256 11.1 | 7.1; 2048 11.6 | 13.0; 2048 dense 40.0 | 26.0; 8192 dense 235 | 241; 4 heads of
+// 8192, W = 2048 42.9 | 35.2; 4096 (16) 51.8 | 53.3.  Backward: N = 1024, W = 256 26.5 | 19.2; 2048 28.3 | 34.2; dense 4096
+// 236 | 194; 8192 567 | 668; d = 128, W = 256: N = 1024 46.1 | 42.5; 2048 50.1 | 80.1; dense 2048 176 | 162, 4096 412 | 502.
+static bool few_tiles(const WindowDims& s, double tiles, double walk, double longest, double c)
+{
+    return tiles * walk < c * longest - (s.D == 64 ? 24000 : 12000);
+}
+static double all_pairs(const WindowDims& s)                 // of one head
+{
+    const double first = s.N - s.q, ramp = std::max<double>(0, std::min<double>(s.W, s.N) - first);
+    return (2 * first + ramp + 1) * ramp / 2 + (s.q - ramp) * s.W;
+}
+bool window_few(const WindowDims& s)
+{
+    const double tiles = (double)s.bh * s.q / 128;
+    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : 230);
+}
 size_t window_few_ws_bytes(const WindowDims& s)
 {
     const int n = few_shares(s);
     return n == 1 ? 0 : a256(sizeof(float) * (size_t)s.bhk * few_groups(s) * n * 32 * (s.D + 2));
 }
 
+template <typename T, int D>
+static size_t few_lds()
+{
+    return kFewWaves * std::max<size_t>(2 * Tile<T, D, kFewKeys>::BYTES, 32 * D * 4);
+}
 template <typename T, int D>
 static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first, void* O,
                         float* lse, void* ws, hipStream_t st)
@@ -276,7 +624,7 @@ static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const
     const int groups = few_groups(s), shares = few_shares(s);
     // keys of a share: whole turns of 32 (the first keys of a group start at a multiple of 32 up to 31 before its own)
     const int each = ((few_keys(s) + 31 + shares - 1) / shares + kFewKeys - 1) / kFewKeys * kFewKeys;
-    constexpr size_t lds = kFewWaves * std::max<size_t>(2 * Tile<T, D, kFewKeys>::BYTES, 32 * D * 4);
+    const size_t lds = few_lds<T, D>();
     auto* kernel = window_few_kernel<T, D>;
     const hipError_t g = ensure_dynamic_lds((const void*)kernel, lds);
     if (g != hipSuccess) return g;
@@ -287,6 +635,61 @@ static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const
     hipLaunchKernelGGL((window_merge_kernel<T, D>), dim3((unsigned)(s.bh * s.q)), dim3(kFewWaves * kWave), 0, st, a, (const T*)Q,
                        (const T*)K, (const T*)V, (T*)O, lse, (const float*)ws, groups, shares);
     return hipGetLastError();
+}
+
+template <typename T, int D>
+static hipError_t few_dq_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO,
+                           const int32_t* first, void* dQ, float* Dv, hipStream_t st)
+{
+    const hipError_t e = ensure_dynamic_lds((const void*)window_few_dq_kernel<T, D>, few_lds<T, D>());
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((window_few_dq_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, few_groups(s))), dim3(kFewWaves * kWave),
+                       (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO,
+                       (T*)dQ, Dv, few_groups(s));
+    return hipGetLastError();
+}
+template <typename T, int D>
+static hipError_t few_dkdv_t(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
+                             const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st)
+{
+    const hipError_t e = ensure_dynamic_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>());
+    if (e != hipSuccess) return e;
+    const int ktiles = (s.N + 31) / 32;
+    hipLaunchKernelGGL((window_few_dkdv_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(kFewWaves * kWave),
+                       (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV,
+                       Dv, ktiles);
+    return hipGetLastError();
+}
+
+bool window_few_dq(const WindowDims& s)
+{
+    const double tiles = (double)s.bh * s.q / 128;
+    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : s.dtype == MOBA_BF16 ? 170 : 230);
+}
+bool window_few_dkdv(const WindowDims& s)
+{
+    const double tiles = (double)s.bhk * s.N / 128;
+    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.N, std::min(s.q, s.W), s.D == 64 ? 325 : s.dtype == MOBA_BF16 ? 170 : 230);
+}
+
+hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
+                                const void* dO, const int32_t* first, void* dQ, float* Dv, hipStream_t st)
+{
+    if (s.dtype == MOBA_BF16)
+        return s.D == 64 ? few_dq_t<bf16_t, 64>(s, Q, K, V, O, lse, dO, first, dQ, Dv, st)
+                         : few_dq_t<bf16_t, 128>(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);
+    return s.D == 64 ? few_dq_t<float, 64>(s, Q, K, V, O, lse, dO, first, dQ, Dv, st)
+                     : few_dq_t<float, 128>(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);
+}
+
+hipError_t launch_window_few_dkdv(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
+                                  const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st)
+{
+    if (s.dtype == MOBA_BF16)
+        return s.D == 64 ? few_dkdv_t<bf16_t, 64>(s, Q, K, V, lse, dO, first, dK, dV, Dv, st)
+                         : few_dkdv_t<bf16_t, 128>(s, Q, K, V, lse, dO, first, dK, dV, Dv, st);
+    return s.D == 64 ? few_dkdv_t<float, 64>(s, Q, K, V, lse, dO, first, dK, dV, Dv, st)
+                     : few_dkdv_t<float, 128>(s, Q, K, V, lse, dO, first, dK, dV, Dv, st);
 }
 
 hipError_t launch_window_few(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first, void* O,
