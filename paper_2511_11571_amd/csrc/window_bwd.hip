@@ -70,18 +70,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     const bool mine = r0 + m32 < a.q;
     if (mine && h == 0) Dv[row] = Dr;
     const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
-    const int lo_min = r0 < a.q ? wave_min_i(lo <= t ? lo : 0x7fffffff) : 0x7fffffff, lo_max = wave_max_i(lo);
-    const int t_min = t0 + min(r0, a.q - 1), t_max = t0 + min(r0 + 31, a.q - 1);
-    if (lane == 0) {
-        wg_lo[wave] = lo_min;
-        if (lo_out && s % a.heads == 0 && r0 < a.q) lo_out[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(lo_min, lo_max);
-    }
-    __syncthreads();
-    int begin = wg_lo[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
-    begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
-    const int end = t0 + min((tile + 1) * QT, a.q);
+    const WaveKeys w = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_lo);
+    if (lo_out && lane == 0 && s % a.heads == 0 && r0 < a.q)
+        lo_out[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(w.lo_min, w.lo_max);
+    const int begin = w.begin, end = t0 + min((tile + 1) * QT, a.q);
 
     f32x16_t acc[MT];
 #pragma unroll
@@ -134,8 +126,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
-                if (u > t_max || u + 31 < lo_min) continue;
-                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min, u < lo_max);
+                if (u > w.t_max || u + 31 < w.lo_min) continue;
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > w.t_min, u < w.lo_max);
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();

@@ -78,8 +78,9 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     Opnd<T> q[STEPS];
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) load_opnd(q[e], Q + ((int64_t)s * a.q + r) * D + 16 * e + 8 * h);
-    const int lo_min = wave_min_i(lo <= t ? lo : 0x7fffffff), lo_max = wave_max_i(lo);
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
+    const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
+    const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
     // the share's keys: a stretch of those that the group's rows can see by their positions
     const int from = max(0, t_min - a.W + 1) / kFewKeys * kFewKeys;
     const int first = max(from + share * each, lo_min == 0x7fffffff ? t_max + 1 : lo_min / kFewKeys * kFewKeys);
@@ -314,8 +315,9 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dq_kernel(Wind
     Dr = sum_halves(Dr);
     if (wave == 0 && h == 0 && 32 * group + m32 < rows) Dv[row] = Dr;
     const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
-    const int lo_min = wave_min_i(lo <= t ? lo : 0x7fffffff), lo_max = wave_max_i(lo);
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
+    const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
+    const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
     unsigned char* mine = smem + wave * WAVE_BYTES;
     f32x16_t acc[MT];
 #pragma unroll

@@ -1,6 +1,6 @@
 // Causal attention to the last W keys: forward.
 //
-// A workgroup takes a tile of neighbouring queries of one head, a wave 32 CT of them, and walks the keys that
+// A workgroup takes a tile of neighbouring queries of one head, a wave 32 of them, and walks the keys that
 // some of them attend in tiles of KT rows through LDS; the next tile is on its way from memory meanwhile.  Scores
 // are computed transposed, S^T = K Q^T, so that a lane holds a query's scores of half the keys and the softmax's
 // maximum and sum cost one exchange of halves; O^T = V^T P^T takes P as it comes out.  Statistics and sums
@@ -12,12 +12,12 @@
 
 namespace moba {
 
-template <typename T, int D, int CT, int NW, int KT, int OCC>
+template <typename T, int D, int NW, int KT, int OCC>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
                                                                    const T* __restrict__ K, const T* __restrict__ V,
                                                                    T* __restrict__ O, float* __restrict__ lse, int ntiles)
 {
-    constexpr int NT = NW * kWave, QT = 32 * CT * NW, STEPS = D / 16, MT = D / 32;
+    constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
     using KV = Tile<T, D, KT>;
     extern __shared__ __align__(16) unsigned char smem[];    // K, V | K, V
     __shared__ int wg_lo[NW];
@@ -28,94 +28,63 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     const int tile = ntiles - 1 - pos / a.G, s = skv * a.G + pos % a.G;      // the longest rows first
     const T* Ks = K + (int64_t)skv * a.rows * D;
     const T* Vs = V + (int64_t)skv * a.rows * D;
-    const int t0 = a.N - a.q, r0 = tile * QT + wave * 32 * CT;
-    int lo[CT], t[CT];
-    Opnd<T> q[CT][STEPS];
-    int lo_min = 0x7fffffff, lo_max = 0;
+    const int t0 = a.N - a.q, r0 = tile * QT + wave * 32;
+    const int r = min(r0 + m32, a.q - 1), t = t0 + r, lo = window_first(a, s, r);            // (rows past the end: the last one again, not stored)
+    const int64_t row = (int64_t)s * a.q + r;
+    Opnd<T> q[STEPS];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int r = min(r0 + 32 * c + m32, a.q - 1);       // (rows past the end: the last one again, not stored)
-        t[c] = t0 + r;
-        lo[c] = window_first(a, s, r);
-        if (lo[c] <= t[c]) lo_min = min(lo_min, lo[c]);
-        lo_max = max(lo_max, lo[c]);
-#pragma unroll
-        for (int e = 0; e < STEPS; ++e) load_opnd(q[c][e], Q + ((int64_t)s * a.q + r) * D + 16 * e + 8 * h);
-    }
-    // keys of the wave's rows: from lo_min to t_max, all rows attend those from lo_max to t_min
-    lo_min = r0 < a.q ? wave_min_i(lo_min) : 0x7fffffff;
-    lo_max = wave_max_i(lo_max);
-    const int t_min = t0 + min(r0, a.q - 1), t_max = t0 + min(r0 + 32 * CT - 1, a.q - 1);
-    if (lane == 0) wg_lo[wave] = lo_min;
-    __syncthreads();
-    int begin = wg_lo[0];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
-    begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
-    const int end = t0 + min((tile + 1) * QT, a.q);          // (begin beyond it: nobody attends anything)
+    for (int e = 0; e < STEPS; ++e) load_opnd(q[e], Q + row * D + 16 * e + 8 * h);
+    const WaveKeys k = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_lo);
+    const int begin = k.begin, end = t0 + min((tile + 1) * QT, a.q);         // (begin beyond it: nobody attends anything)
 
     const float c2 = a.scale * kLog2e;
-    f32x16_t acc[CT][MT];
-    float ref[CT], l[CT];
+    f32x16_t acc[MT];
+    float ref = kLowest, l = 0.f;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        ref[c] = kLowest;
-        l[c] = 0.f;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[c][mt] = f32x16_t{};
-    }
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
     auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) __attribute__((always_inline)) {
-        f32x16_t S[CT];
-#pragma unroll
-        for (int c = 0; c < CT; ++c) S[c] = f32x16_t{};
+        f32x16_t S = f32x16_t{};
 #pragma unroll
         for (int e = 0; e < STEPS; ++e) {
-            Opnd<T> k;
-            KV::rows(k, kt, row0, e, h, m32);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) S[c] = mma(k, q[c][e], S[c]);
+            Opnd<T> x;
+            KV::rows(x, kt, row0, e, h, m32);
+            S = mma(x, q[e], S);
         }
-        Opnd<T> p[CT][2];
+        float x[16];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            float x[16];
+        for (int i = 0; i < 16; ++i) x[i] = S[i];
+        if (late) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = S[c][i];
-            if (late) {
-                const int most = t[c] - u - 4 * h;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= most ? x[i] : -INFINITY;
-            }
-            if (early) {
-                const int least = lo[c] - u - 4 * h;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= least ? x[i] : -INFINITY;
-            }
-            float top = x[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
-            top = max_halves(top) * c2;
-            if (__ballot(top > ref[c] + 8.f)) {
-                const float now = fmaxf(ref[c], top), alpha = fast_exp2(ref[c] - now);
-                ref[c] = now;
-                l[c] *= alpha;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) acc[c][mt] *= alpha;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref[c]));
-            l[c] += sum16(x);
-            pack_opnd(p[c][0], x);
-            pack_opnd(p[c][1], x + 8);
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) <= t - u - 4 * h ? x[i] : -INFINITY;
         }
+        if (early) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = max_nan(top, x[i]);
+        top = max_halves(top) * c2;
+        if (__ballot(top > ref + 8.f)) {
+            const float now = fmaxf(ref, top), alpha = fast_exp2(ref - now);
+            ref = now;
+            l *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[mt] *= alpha;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref));
+        l += sum16(x);
+        Opnd<T> p[2];
+        pack_opnd(p[0], x);
+        pack_opnd(p[1], x + 8);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 Opnd<T> v;
                 KV::cols(v, vt, row0 + 16 * j, mt, lane);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) acc[c][mt] = mma(v, p[c][j], acc[c][mt]);
+                acc[mt] = mma(v, p[j], acc[mt]);
             }
     };
     if (begin < end) {
@@ -131,8 +100,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
-                if (u > t_max || u + 31 < lo_min) continue;
-                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > t_min, u < lo_max);
+                if (u > k.t_max || u + 31 < k.lo_min) continue;
+                keys32(kt, kt + KV::BYTES, 32 * x, u, u + 31 > k.t_min, u < k.lo_max);
             }
             if (u0 + KT < end) next.finish(to, tid);
             __syncthreads();
@@ -142,51 +111,45 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
             if (u0 + KT < end) step(u0 + KT, std::integral_constant<int, 1>());
         }
     }
-    if (r0 >= a.q) return;
+    const bool empty = lo > t;
+    const float L = sum_halves(l), inv = empty ? 0.f : 1.f / L;
+    bool odd = false;                                        // a result that is not finite
+    if (r0 + m32 < a.q) {
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int r = r0 + 32 * c + m32;
-        const int64_t row = (int64_t)s * a.q + r;
-        const bool empty = lo[c] > t[c];
-        const float L = sum_halves(l[c]), inv = empty ? 0.f : 1.f / L;
-        bool odd = false;                                    // a result that is not finite
-        if (r < a.q) {
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int i = 0; i < 16; i += 4) {
+                float o[4];
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    float o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        o[e] = empty ? 0.f : acc[c][mt][i + e] * inv;
-                        odd |= !(fabsf(o[e]) < INFINITY);
-                    }
-                    T* to = O + row * D + 32 * mt + result_row(i) + 4 * h;
-                    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-                    else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = empty ? 0.f : acc[mt][i + e] * inv;
+                    odd |= !(fabsf(o[e]) < INFINITY);
                 }
-            if (h == 0) lse[row] = empty ? -INFINITY : (ref[c] + fast_log2(L)) * kLn2;
-        }
-        // A weight of zero does not hide an infinity or a NaN: such rows are done once more, from their own pairs alone
-        uint64_t bad = __ballot(odd);
-        bad = (bad | bad >> 32) & 0xffffffffu;
-        for (; bad; bad &= bad - 1) plain_forward_row<T, D>(a, Q, K, V, O, lse, s, r0 + 32 * c + __builtin_ctzll(bad), lane);
+                T* to = O + row * D + 32 * mt + result_row(i) + 4 * h;
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
+                else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+            }
+        if (h == 0) lse[row] = empty ? -INFINITY : (ref + fast_log2(L)) * kLn2;
     }
+    // A weight of zero does not hide an infinity or a NaN: such rows are done once more, from their own pairs alone
+    uint64_t bad = __ballot(odd);
+    bad = (bad | bad >> 32) & 0xffffffffu;
+    for (; bad; bad &= bad - 1) plain_forward_row<T, D>(a, Q, K, V, O, lse, s, r0 + __builtin_ctzll(bad), lane);
 }
 
 size_t window_forward_ws_bytes(const WindowDims& s) { return window_few(s) ? window_few_ws_bytes(s) : 0; }
 
-template <typename T, int D, int CT, int NW, int KT, int OCC>
+template <typename T, int D, int NW, int KT, int OCC>
 static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                           void* O, float* lse, hipStream_t st)
 {
-    auto* kernel = window_forward_kernel<T, D, CT, NW, KT, OCC>;
+    auto* kernel = window_forward_kernel<T, D, NW, KT, OCC>;
     constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
     if (lds > 64 * 1024) {
         const hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
     }
-    constexpr int QT = 32 * CT * NW;
+    constexpr int QT = 32 * NW;
     const int ntiles = (s.q + QT - 1) / QT;
     hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, s.G * ntiles)), dim3(NW * kWave), lds, st,
                        window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (T*)O, lse, ntiles);
@@ -198,10 +161,10 @@ hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void*
 {
     if (window_few(s)) return launch_window_few(s, Q, K, V, first, O, lse, ws, st);
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? tiles_t<bf16_t, 64, 1, 4, 64, 4>(s, Q, K, V, first, O, lse, st)
-                         : tiles_t<bf16_t, 128, 1, 4, 64, 2>(s, Q, K, V, first, O, lse, st);
-    return s.D == 64 ? tiles_t<float, 64, 1, 4, 32, 3>(s, Q, K, V, first, O, lse, st)
-                     : tiles_t<float, 128, 1, 4, 32, 2>(s, Q, K, V, first, O, lse, st);
+        return s.D == 64 ? tiles_t<bf16_t, 64, 4, 64, 4>(s, Q, K, V, first, O, lse, st)
+                         : tiles_t<bf16_t, 128, 4, 64, 2>(s, Q, K, V, first, O, lse, st);
+    return s.D == 64 ? tiles_t<float, 64, 4, 32, 3>(s, Q, K, V, first, O, lse, st)
+                     : tiles_t<float, 128, 4, 32, 2>(s, Q, K, V, first, O, lse, st);
 }
 
 }  // namespace moba

@@ -183,6 +183,34 @@ __device__ __forceinline__ int wave_min_i(int x)
 }
 __device__ __forceinline__ int wave_max_i(int x) { return -wave_min_i(-x); }
 
+// Keys that a wave's 32 rows from r0 on attend: some of them those from lo_min to t_max, all of them those from lo_max to
+// t_min; begin: a multiple of 32 that is not behind the first key of the workgroup, whose rows start at wg_r0.
+struct WaveKeys {
+    int lo_min, lo_max, t_min, t_max, begin;
+};
+template <int NW>
+__device__ __forceinline__ WaveKeys wave_keys(const WindowArgs& a, int t0, int wg_r0, int r0, int t, int lo, int wave, int lane, int* wg_lo)
+{
+    WaveKeys k;
+    k.t_min = t0 + min(r0, a.q - 1);
+    k.t_max = t0 + min(r0 + 31, a.q - 1);
+    if (!a.first) {                                          // first keys rise with the rows
+        k.lo_min = r0 < a.q ? max(0, k.t_min - a.W + 1) : 0x7fffffff;
+        k.lo_max = max(0, k.t_max - a.W + 1);
+        k.begin = max(0, t0 + wg_r0 - a.W + 1) & ~31;
+        return k;
+    }
+    k.lo_min = r0 < a.q ? wave_min_i(lo <= t ? lo : 0x7fffffff) : 0x7fffffff;
+    k.lo_max = wave_max_i(lo);
+    if (lane == 0) wg_lo[wave] = k.lo_min;
+    __syncthreads();
+    int begin = wg_lo[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
+    k.begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
+    return k;
+}
+
 // row of a result's element i
 __device__ __forceinline__ constexpr int result_row(int i) { return 8 * (i >> 2) + (i & 3); }
 
