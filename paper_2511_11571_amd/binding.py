@@ -471,46 +471,67 @@ def window_workspace_bytes(shape: WindowShape):
     return n
 
 
-def _window_args(shape, first_key, *tensors):
-    b, d, dt, dev = shape.batch, shape.head_dim, shape.torch_dtype, torch._C._cuda_getDevice()
-    for t, heads, rows in tensors:
-        assert t.is_contiguous() and t.dtype == dt and t.shape == (b, heads, rows, d) and t.get_device() == dev
-    if first_key is not None:
-        assert (first_key.is_contiguous() and first_key.dtype == torch.int32 and first_key.shape == (b, shape.q_len) and
-                first_key.get_device() == dev)
+def _sizes(shape):
+    """What a call's tensors are compared with, put together once per (immutable) shape."""
+    n = shape.__dict__.get("_tensor_sizes")
+    if n is None:
+        b, h, hkv, d = shape.batch, shape.heads, shape.hkv, shape.head_dim
+        if isinstance(shape, WindowShape):
+            n = ((b, h, shape.q_len, d), (b, hkv, shape.rows, d), (b, h, shape.q_len), (b, shape.q_len), shape.torch_dtype)
+        else:
+            q, k = shape.q_out_rows or shape.seqlen, shape.k_out_rows or shape.seqlen
+            n = ((b, h, shape.seqlen, d), (b, hkv, shape.seqlen, d), (b, h, q, d), (b, hkv, k, d), shape.torch_dtype,
+                 not (shape.q_rows or shape.k_rows))
+        shape.__dict__["_tensor_sizes"] = n
+    return n
+
+
+def _is(t, size, dtype, dev):
+    return t.dtype is dtype and t.shape == size and t.is_contiguous() and t.get_device() == dev
 
 
 def window_forward(shape: WindowShape, Q, K, V, first_key=None, ws=None, O=None, lse=None):
     """-> (O [b,h,q_len,d], lse [b,h,q_len] fp32).  K, V: [b,kv,rows,d].  first_key: [b,q_len] int32, the first key
     of the sequence that every row belongs to (VarlenLayout.first_key), or None."""
-    h, q = shape.heads, shape.q_len
-    _window_args(shape, first_key, (Q, h, q), (K, shape.hkv, shape.rows), (V, shape.hkv, shape.rows))
+    qs, ks, ls, fs, dt = _sizes(shape)
+    dev = torch._C._cuda_getDevice()
+    assert _is(Q, qs, dt, dev) and _is(K, ks, dt, dev) and _is(V, ks, dt, dev)
+    assert first_key is None or _is(first_key, fs, torch.int32, dev)
     if O is None:
         O = torch.empty_like(Q)
+    else:
+        assert _is(O, qs, dt, dev)
     if lse is None:
-        lse = Q.new_empty(Q.shape[:3], dtype=torch.float32)
+        lse = Q.new_empty(ls, dtype=torch.float32)
+    else:
+        assert _is(lse, ls, torch.float32, dev)
     if ws is None:
         need = window_workspace_bytes(shape)[0]
         ws = _ws(need, Q) if need else None
-    assert lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == Q.shape[:3] and lse.device == Q.device
-    _window_args(shape, None, (O, h, q))
-    assert ws is None or (ws.is_contiguous() and ws.dtype == torch.uint8 and ws.device == Q.device)
-    _check(_fn("moba_window_forward", "p" * 8 + "zp")(shape._ref(), Q.data_ptr(), K.data_ptr(), V.data_ptr(), _p(first_key),
-                                                    O.data_ptr(), lse.data_ptr(), _p(ws),
-                                                    0 if ws is None else ws.numel(), _stream()), "moba_window_forward")
+    else:
+        assert ws.is_contiguous() and ws.dtype is torch.uint8 and ws.get_device() == dev
+    _check(_fn("moba_window_forward", "p" * 8 + "zp")(
+        shape._ref(), Q.data_ptr(), K.data_ptr(), V.data_ptr(), _p(first_key), O.data_ptr(), lse.data_ptr(), _p(ws),
+        0 if ws is None else ws.numel(), _stream()), "moba_window_forward")
     return O, lse
 
 
 def window_backward(shape: WindowShape, Q, K, V, O, lse, dO, first_key=None, ws=None, out=None):
     """-> (dQ [b,h,q_len,d], dK, dV [b,kv,rows,d]).  Rows of dK and dV from kv_len on are not written."""
-    h, q, hkv, rows = shape.heads, shape.q_len, shape.hkv, shape.rows
-    _window_args(shape, first_key, (Q, h, q), (K, hkv, rows), (V, hkv, rows), (O, h, q), (dO, h, q))
-    assert lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == Q.shape[:3] and lse.device == Q.device
-    dQ, dK, dV = out if out is not None else (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V))
-    _window_args(shape, None, (dQ, h, q), (dK, hkv, rows), (dV, hkv, rows))
+    qs, ks, ls, fs, dt = _sizes(shape)
+    dev = torch._C._cuda_getDevice()
+    assert _is(Q, qs, dt, dev) and _is(K, ks, dt, dev) and _is(V, ks, dt, dev) and _is(O, qs, dt, dev)
+    assert _is(dO, qs, dt, dev) and _is(lse, ls, torch.float32, dev)
+    assert first_key is None or _is(first_key, fs, torch.int32, dev)
+    if out is None:
+        dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)
+    else:
+        dQ, dK, dV = out
+        assert _is(dQ, qs, dt, dev) and _is(dK, ks, dt, dev) and _is(dV, ks, dt, dev)
     if ws is None:
         ws = _ws(window_workspace_bytes(shape)[1], Q)
-    assert ws.is_contiguous() and ws.dtype == torch.uint8 and ws.device == Q.device
+    else:
+        assert ws.is_contiguous() and ws.dtype is torch.uint8 and ws.get_device() == dev
     _check(_fn("moba_window_backward", "p" * 12 + "zp")(
         shape._ref(), Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
         _p(first_key), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
@@ -518,25 +539,37 @@ def window_backward(shape: WindowShape, Q, K, V, O, lse, dO, first_key=None, ws=
     return dQ, dK, dV
 
 
+def _rope_rows(t, heads, rows, shape, dt, dev):
+    """[b, heads, N or more rows, d] with ``rows`` rows per slice in memory (0: N): a tensor, or a stretch of a larger
+    one's rows, such as a cache's."""
+    n, d, size, st = shape.seqlen, shape.head_dim, t.shape, t.stride()
+    rows = rows or n
+    return (t.dtype is dt and t.dim() == 4 and size[0] == shape.batch and size[1] == heads and size[3] == d and
+            n <= size[2] <= rows and st[3] == 1 and (size[2] == 1 or st[2] == d) and (heads == 1 or st[1] == rows * d) and
+            (shape.batch == 1 or st[0] == heads * rows * d) and t.get_device() == dev)
+
+
 def _rope(name, shape, Q, K, positions, out):
-    b, n, d, dt, dev = shape.batch, shape.seqlen, shape.head_dim, shape.torch_dtype, torch._C._cuda_getDevice()
+    qs, ks, qo, ko, dt, packed = _sizes(shape)
+    dev = torch._C._cuda_getDevice()
+    if packed:
+        assert _is(Q, qs, dt, dev) or _rope_rows(Q, shape.heads, 0, shape, dt, dev)
+        assert K is None or _is(K, ks, dt, dev) or _rope_rows(K, shape.hkv, 0, shape, dt, dev)
+    else:
+        assert _rope_rows(Q, shape.heads, shape.q_rows, shape, dt, dev)
+        assert K is None or _rope_rows(K, shape.hkv, shape.k_rows, shape, dt, dev)
     Qo, Ko = out if out is not None else (None, None)
     if Qo is None:
-        Qo = Q.new_empty((b, shape.heads, shape.q_out_rows or n, d))
-    if Ko is None and K is not None:
-        Ko = K.new_empty((b, shape.hkv, shape.k_out_rows or n, d))
-    for t, heads, rows in ((Q, shape.heads, shape.q_rows), (Qo, shape.heads, shape.q_out_rows),
-                           (K, shape.hkv, shape.k_rows), (Ko, shape.hkv, shape.k_out_rows)):
-        # (a stretch of a cache's rows is a view with the cache's own stride)
-        if t is not None:
-            rows = rows or n
-            size, st = t.shape, t.stride()
-            assert t.dtype == dt and t.dim() == 4 and size[:2] == (b, heads) and size[3] == d and t.get_device() == dev
-            assert n <= size[2] <= rows and st[3] == 1 and (size[2] == 1 or st[2] == d)
-            assert (heads == 1 or st[1] == rows * d) and (b == 1 or st[0] == heads * rows * d)
-    if positions is not None:
-        assert (positions.is_contiguous() and positions.dtype == torch.int32 and positions.shape == (b, n) and
-                positions.get_device() == dev)
+        Qo = Q.new_empty(qo)
+    else:
+        assert _rope_rows(Qo, shape.heads, shape.q_out_rows, shape, dt, dev)
+    if K is None:
+        assert Ko is None
+    elif Ko is None:
+        Ko = K.new_empty(ko)
+    else:
+        assert _rope_rows(Ko, shape.hkv, shape.k_out_rows, shape, dt, dev)
+    assert positions is None or _is(positions, (shape.batch, shape.seqlen), torch.int32, dev)
     _check(_fn(name, "ppppppp")(shape._ref(), Q.data_ptr(), _p(K), _p(positions), Qo.data_ptr(), _p(Ko), _stream()), name)
     return Qo, Ko
 

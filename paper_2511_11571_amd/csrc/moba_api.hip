@@ -263,8 +263,12 @@ int rope_args(const moba_rope_shape* sh, RopeArgs& a)
     a.yrows[0] = rows(sh->q_out_rows);
     a.yrows[1] = rows(sh->k_out_rows);
     const double two_pi = 6.283185307179586476925;
+    // theta^(-2 i / rot) as a product of two powers: sixteen of them for a call instead of sixty-four
+    double low[8], high[kRopeMaxPairs / 8];
+    for (int i = 0; i < 8; ++i) low[i] = pow(sh->theta, -2.0 * i / a.rot);
+    for (int i = 0; 8 * i < a.rot / 2; ++i) high[i] = pow(sh->theta, -16.0 * i / a.rot);
     for (int i = 0; i < a.rot / 2; ++i) {
-        double f = pow(sh->theta, -2.0 * i / a.rot);
+        double f = high[i / 8] * low[i % 8];
         if (sh->scale_factor != 1.0) {
             double keep = 0.0;
             if (sh->orig_len > 0.0) {

@@ -16,6 +16,9 @@ struct WindowDims {
     float scale;
 };
 
+// dynamic LDS of a kernel, beyond what every launch may have
+inline hipError_t window_lds(const void* kernel, size_t bytes) { return bytes > 64 * 1024 ? ensure_dynamic_lds(kernel, bytes) : hipSuccess; }
+
 // what a kernel needs of it
 struct WindowArgs {
     int q, N, rows, W, G, heads, bhk;

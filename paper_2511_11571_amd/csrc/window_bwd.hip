@@ -376,7 +376,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     } else {
         constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
         auto* kernel = window_dq_kernel<T, D, NW, KT, OCCQ>;
-        e = ensure_dynamic_lds((const void*)kernel, lds);
+        e = window_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
         const int tiles = (s.q + 32 * NW - 1) / (32 * NW);
         hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, s.G * tiles)), dim3(NW * kWave), lds, st, a, (const T*)Q,
@@ -393,7 +393,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     }
     constexpr size_t lds = 4 * Tile<T, D, QT>::BYTES;
     auto* kernel = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT>;
-    e = ensure_dynamic_lds((const void*)kernel, lds);
+    e = window_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     const int tiles = (s.N + 32 * NW - 1) / (32 * NW);
     hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, tiles)), dim3(NW * kWave), lds, st, a, (const T*)Q, (const T*)K,

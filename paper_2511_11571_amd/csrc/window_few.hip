@@ -628,7 +628,7 @@ static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const
     const int each = ((few_keys(s) + 31 + shares - 1) / shares + kFewKeys - 1) / kFewKeys * kFewKeys;
     const size_t lds = few_lds<T, D>();
     auto* kernel = window_few_kernel<T, D>;
-    const hipError_t g = ensure_dynamic_lds((const void*)kernel, lds);
+    const hipError_t g = window_lds((const void*)kernel, lds);
     if (g != hipSuccess) return g;
     hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, groups * shares)), dim3(kFewWaves * kWave), lds, st, a,
                        (const T*)Q, (const T*)K, (const T*)V, (T*)O, lse, (float*)ws, groups, shares, each);
@@ -643,7 +643,7 @@ template <typename T, int D>
 static hipError_t few_dq_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO,
                            const int32_t* first, void* dQ, float* Dv, hipStream_t st)
 {
-    const hipError_t e = ensure_dynamic_lds((const void*)window_few_dq_kernel<T, D>, few_lds<T, D>());
+    const hipError_t e = window_lds((const void*)window_few_dq_kernel<T, D>, few_lds<T, D>());
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((window_few_dq_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, few_groups(s))), dim3(kFewWaves * kWave),
                        (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO,
@@ -654,7 +654,7 @@ template <typename T, int D>
 static hipError_t few_dkdv_t(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
                              const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st)
 {
-    const hipError_t e = ensure_dynamic_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>());
+    const hipError_t e = window_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>());
     if (e != hipSuccess) return e;
     const int ktiles = (s.N + 31) / 32;
     hipLaunchKernelGGL((window_few_dkdv_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(kFewWaves * kWave),

@@ -145,10 +145,8 @@ static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, con
 {
     auto* kernel = window_forward_kernel<T, D, NW, KT, OCC>;
     constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
-    if (lds > 64 * 1024) {
-        const hipError_t e = ensure_dynamic_lds((const void*)kernel, lds);
-        if (e != hipSuccess) return e;
-    }
+    const hipError_t e = window_lds((const void*)kernel, lds);
+    if (e != hipSuccess) return e;
     constexpr int QT = 32 * NW;
     const int ntiles = (s.q + QT - 1) / QT;
     hipLaunchKernelGGL(kernel, dim3((unsigned)schedule_grid(s.bhk, s.G * ntiles)), dim3(NW * kWave), lds, st,
