@@ -56,6 +56,28 @@ def test_forward_and_backward(case, dt, d):
     _check(_shape(b, h, hkv, q, N, d, W, dt), Q, K, V, dO)
 
 
+# enough tiles of queries, or of keys, for the kernels that work tile by tile: both of them; with shared heads; dense; fewer
+# queries than keys; queries by tiles and keys not (heads that share); the other way round (few queries)
+TILES = [
+    (2, 70, 70, 131, 131, 40), (2, 128, 64, 131, 131, 33), (1, 264, 264, 200, 200, 0), (1, 200, 200, 100, 300, 45),
+    (1, 300, 300, 257, 257, 256), (1, 256, 16, 131, 131, 40), (1, 200, 200, 20, 300, 45), (3, 50, 50, 129, 129, 1),
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("case", TILES, ids=str)
+def test_forward_and_backward_tile_by_tile(case, dt, d):
+    b, h, hkv, q, N, W = case
+    Q, K, V, dO = _draw(sum(case) + d, b, h, hkv, q, N, d, dt)
+    first = None
+    if (q + W) % 2:                                          # half of them with sequences that start on the way
+        g = torch.Generator().manual_seed(q)
+        starts = torch.randint(0, 2, (b, q), generator=g).cumsum(1) * 7
+        first = torch.minimum(starts.to(torch.int32), torch.arange(N - q, N, dtype=torch.int32)).cuda()
+    _check(_shape(b, h, hkv, q, N, d, W, dt), Q, K, V, dO, first)
+
+
 # the last few positions against a long cache: few queries, keys shared out among workgroups
 TOKENS = [
     (1, 1, 1, 1, 2000, 0), (2, 4, 2, 1, 4097, 0), (1, 16, 4, 4, 3001, 0), (1, 8, 1, 7, 5000, 1000), (3, 2, 2, 16, 2500, 256),
@@ -71,13 +93,18 @@ def test_few_tokens_against_a_cache_with_room(case, dt, d):
     rows = N + 61
     Q, K, V, _ = _draw(sum(case), b, h, hkv, q, rows, d, dt)
     K[:, :, N:], V[:, :, N:] = float("nan"), float("inf")    # rows behind the last key are not read
-    _check(_shape(b, h, hkv, q, N, d, W, dt, rows), Q, K, V)
+    sh = _shape(b, h, hkv, q, N, d, W, dt, rows)
+    _check(sh, Q, K, V)
+    # sequences of a padded batch that begin late, in the middle of a share or behind all keys
+    first = torch.tensor([[0, N - 1, N // 2 + 3, N][(i + r) % 4] for i in range(b) for r in range(q)], dtype=torch.int32).view(b, q).cuda()
+    _check(sh, Q, K, V, first=first)
 
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-def test_packed_batch_is_each_sequence_on_its_own(dt, d):
-    lens, W, h, hkv = [1, 130, 64, 0, 77, 200], 96, 4, 2
+@pytest.mark.parametrize("h,hkv,W", [(4, 2, 96), (64, 64, 40)])
+def test_packed_batch_is_each_sequence_on_its_own(h, hkv, W, dt, d):
+    lens = [1, 130, 64, 0, 77, 200]
     offs = np.concatenate([[0], np.cumsum(lens)])
     N = int(offs[-1])
     lay = moba.VarlenLayout([int(x) for x in offs], 32)
@@ -100,11 +127,11 @@ def test_packed_batch_is_each_sequence_on_its_own(dt, d):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("W", [0, 50])
-def test_rows_that_attend_nothing(dt, d, W):
+@pytest.mark.parametrize("h,hkv,W", [(2, 1, 0), (2, 1, 50), (36, 36, 40)])
+def test_rows_that_attend_nothing(dt, d, h, hkv, W):
     """A padded batch: rows of padding attend nothing, whatever they hold, and rows in no order of first keys."""
-    b, h, N = 3, 2, 230
-    Q, K, V, dO = _draw(5, b, h, 1, N, N, d, dt)
+    b, N = 3, 230
+    Q, K, V, dO = _draw(5, b, h, hkv, N, N, d, dt)
     first = torch.zeros((b, N), dtype=torch.int32)
     first[0, :70], first[0, 70:] = 1 << 30, 70               # padding on the left
     first[1, 100:] = N                                       # and on the right
@@ -112,15 +139,15 @@ def test_rows_that_attend_nothing(dt, d, W):
     first = first.cuda()
     off = first > torch.arange(N, device="cuda")
     bad = off[:, None].expand(b, h, N)
-    O, lse, (dQ, dK, dV) = _check(_shape(b, h, 1, N, N, d, W, dt), Q, K, V, dO, first)
+    O, lse, (dQ, dK, dV) = _check(_shape(b, h, hkv, N, N, d, W, dt), Q, K, V, dO, first)
     assert (O[bad] == 0).all() and (lse[bad] == -float("inf")).all() and (dQ[bad] == 0).all()
     # the same with rubbish in those rows, and in keys that nobody attends
     Q2, dO2, K2, V2 = Q.clone(), dO.clone(), K.clone(), V.clone()
     Q2[bad], dO2[bad] = float("nan"), float("inf")
-    nobody = torch.from_numpy(~ref.seen(N, N, W, first.cpu().numpy(), b).any(1)).cuda()[:, None]
+    nobody = torch.from_numpy(~ref.seen(N, N, W, first.cpu().numpy(), b).any(1)).cuda()[:, None].expand(b, hkv, N)
     assert nobody.any()
     K2[nobody], V2[nobody] = float("inf"), float("nan")
-    sh = _shape(b, h, 1, N, N, d, W, dt)
+    sh = _shape(b, h, hkv, N, N, d, W, dt)
     O2, lse2 = moba.window_forward(sh, Q2, K2, V2, first_key=first)
     g2 = moba.window_backward(sh, Q2, K2, V2, O2, lse2, dO2, first_key=first)
     want = ref.window(Q2, K2, V2, W, first, dO=dO2)
@@ -130,8 +157,9 @@ def test_rows_that_attend_nothing(dt, d, W):
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(dt, value):
-    h, N, d, W, at = 2, 300, 64, 40, 117
+@pytest.mark.parametrize("h,d", [(2, 64), (2, 128), (80, 64), (80, 128)])
+def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(h, d, dt, value):
+    N, W, at = 300, 40, 117
     Q, K, V, dO = _draw(8, 1, h, h, N, N, d, dt)
     sh = _shape(1, h, h, N, N, d, W, dt)
     want = ref.window(Q, K, V, W, None, dO=dO)
@@ -146,8 +174,9 @@ def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(dt, value):
         for name, x, rows in zip(("O", "lse", "dQ", "dK", "dV"), (O, lse) + grads, (touched, touched, touched, near, near)):
             value_, bound = want[name]
             keep = ~rows.numpy()
-            ref.close(x[:, :1], (value_[:, :1], bound[:, :1]), name)                 # the other head
-            ref.close(x[:, 1:, keep], (value_[:, 1:, keep], bound[:, 1:, keep]), name)
+            others = [i for i in range(h) if i != 1]
+            ref.close(x[:, others], (value_[:, others], bound[:, others]), name)
+            ref.close(x[:, 1:2, keep], (value_[:, 1:2, keep], bound[:, 1:2, keep]), name)
         if which == "V":
             assert not torch.isfinite(O[0, 1, touched][:, 3]).any()
     # a bad query reaches its own row, and the gradients of the keys that it attends
@@ -159,17 +188,18 @@ def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(dt, value):
     for name, x, rows in (("O", O, mine), ("dQ", dQ, mine), ("dK", dK, seen), ("dV", dV, seen)):
         value_, bound = want[name]
         keep = ~rows.numpy()
-        ref.close(x[:, 1:, keep], (value_[:, 1:, keep], bound[:, 1:, keep]), name)
+        ref.close(x[:, 1:2, keep], (value_[:, 1:2, keep], bound[:, 1:2, keep]), name)
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("scale", [0.3, 1e-4])
-def test_scales_and_large_logits(dt, scale):
+@pytest.mark.parametrize("h,W", [(2, 128), (70, 50)])
+def test_scales_and_large_logits(h, W, dt, scale):
     """Logits of tens to hundreds: the running maximum moves, most weights vanish."""
-    Q, K, V, dO = _draw(9, 1, 2, 2, 260, 260, 64, dt)
+    Q, K, V, dO = _draw(9, 1, h, h, 260, 260, 64, dt)
     K[:, :, 40] *= 6
     K[:, :, 200] *= 9
-    _check(_shape(1, 2, 2, 260, 260, 64, 128, dt, scale=scale), Q, K, V, dO)
+    _check(_shape(1, h, h, 260, 260, 64, W, dt, scale=scale), Q, K, V, dO)
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
@@ -199,11 +229,14 @@ def test_gradients_against_differences(dt):
         assert abs(got - diff) <= float((want[name][1] * v.abs().numpy()).sum()) + 1e-5 * float(v.norm())
 
 
-def test_nothing_outside_the_buffers_is_written():
-    b, h, hkv, N, d, W = 1, 4, 2, 210, 64, 100
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("h,hkv,W", [(4, 2, 100), (90, 90, 40)])
+def test_nothing_outside_the_buffers_is_written(h, hkv, W, d, dt):
+    b, N = 1, 210
     rows, guard = 240, 4096
-    Q, K, V, dO = _draw(12, b, h, hkv, N, rows, d, torch.bfloat16)
-    sh = _shape(b, h, hkv, N, N, d, W, torch.bfloat16, rows)
+    Q, K, V, dO = _draw(12, b, h, hkv, N, rows, d, dt)
+    sh = _shape(b, h, hkv, N, N, d, W, dt, rows)
 
     def room(shape, dtype):
         n = int(np.prod(shape)) * torch.finfo(dtype).bits // 8
@@ -227,7 +260,8 @@ def test_nothing_outside_the_buffers_is_written():
 
 def test_streams_graphs_and_repeats():
     """A captured pass replayed after eager work of the same shapes, and on another stream, gives the same bits."""
-    shapes = [(_shape(1, 4, 2, 400, 400, 64, 90, torch.bfloat16), True), (_shape(1, 8, 2, 2, 3000, 128, 0, torch.bfloat16), False)]
+    shapes = [(_shape(1, 4, 2, 400, 400, 64, 90, torch.bfloat16), True), (_shape(1, 8, 2, 2, 3000, 128, 0, torch.bfloat16), False),
+              (_shape(1, 48, 48, 400, 400, 128, 40, torch.bfloat16), True)]
     for sh, train in shapes:
         q, N = sh.q_len, sh.kv_len
         Q, K, V, dO = _draw(13, 1, sh.heads, sh.hkv, q, N, sh.head_dim, torch.bfloat16)
