@@ -137,7 +137,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             if (u0 + KT < end) step(u0 + KT, std::integral_constant<int, 1>());
         }
     }
-    bool odd = false;
+    float most = 0.f;
     if (mine) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -146,8 +146,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
                 float o[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    o[e] = lo > t ? 0.f : acc[mt][i + e] * a.scale;
-                    odd |= !(fabsf(o[e]) < INFINITY);
+                    o[e] = acc[mt][i + e] * a.scale;
+                    most = max_nan(most, fabsf(o[e]));
                 }
                 T* to = dQ + row * D + 32 * mt + result_row(i) + 4 * h;
                 if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             }
     }
     // rows with a sum that is not finite once more, from their own pairs alone
-    uint64_t bad = __ballot(odd);
+    uint64_t bad = __ballot(!(most < INFINITY));
     bad = (bad | bad >> 32) & 0xffffffffu;
     for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, Dv, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
@@ -330,12 +330,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             if (more) arrived(buf ^ 1);
         }
     }
-    bool odd = false;
+    float most = 0.f;
     if (key < a.N) {
         const int64_t at = ((int64_t)skv * a.rows + key) * D;
         auto store = [&](T* to, const float (&o)[4]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[e]) < INFINITY);
+            for (int e = 0; e < 4; ++e) most = max_nan(most, fabsf(o[e]));
             if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
             else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
         };
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             }
     }
     // keys with a sum that is not finite once more, from their own pairs alone
-    uint64_t bad = __ballot(odd);
+    uint64_t bad = __ballot(!(most < INFINITY));
     bad = (bad | bad >> 32) & 0xffffffffu;
     for (; bad; bad &= bad - 1) plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, left.D, dK, dV, skv, ku + __builtin_ctzll(bad), lane);
 }

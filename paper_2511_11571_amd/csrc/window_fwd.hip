@@ -113,7 +113,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     }
     const bool empty = lo > t;
     const float L = sum_halves(l), inv = empty ? 0.f : 1.f / L;
-    bool odd = false;                                        // a result that is not finite
+    float most = 0.f;
     if (r0 + m32 < a.q) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -122,8 +122,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
                 float o[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    o[e] = empty ? 0.f : acc[mt][i + e] * inv;
-                    odd |= !(fabsf(o[e]) < INFINITY);
+                    o[e] = acc[mt][i + e] * inv;
+                    most = max_nan(most, fabsf(o[e]));
                 }
                 T* to = O + row * D + 32 * mt + result_row(i) + 4 * h;
                 if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
         if (h == 0) lse[row] = empty ? -INFINITY : (ref + fast_log2(L)) * kLn2;
     }
     // A weight of zero does not hide an infinity or a NaN: such rows are done once more, from their own pairs alone
-    uint64_t bad = __ballot(odd);
+    uint64_t bad = __ballot(!(most < INFINITY));
     bad = (bad | bad >> 32) & 0xffffffffu;
     for (; bad; bad &= bad - 1) plain_forward_row<T, D>(a, Q, K, V, O, lse, s, r0 + __builtin_ctzll(bad), lane);
 }
