@@ -140,19 +140,15 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     float most = 0.f;
     if (mine) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+            float o[16];
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                float o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[e] = acc[mt][i + e] * a.scale;
-                    most = max_nan(most, fabsf(o[e]));
-                }
-                T* to = dQ + row * D + 32 * mt + result_row(i) + 4 * h;
-                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-                else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+            for (int i = 0; i < 16; ++i) {
+                o[i] = acc[mt][i] * a.scale;
+                most = max_nan(most, fabsf(o[i]));
             }
+            store_result(dQ + row * D + 32 * mt, o, h);
+        }
     }
     // rows with a sum that is not finite once more, from their own pairs alone
     uint64_t bad = __ballot(!(most < INFINITY));
@@ -333,22 +329,18 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     float most = 0.f;
     if (key < a.N) {
         const int64_t at = ((int64_t)skv * a.rows + key) * D;
-        auto store = [&](T* to, const float (&o)[4]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) most = max_nan(most, fabsf(o[e]));
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-            else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
-        };
+        for (int mt = 0; mt < MT; ++mt) {
+            float x[16], y[16];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int64_t o = at + 32 * mt + result_row(i) + 4 * h;
-                const float x[4] = {ak[mt][i] * a.scale, ak[mt][i + 1] * a.scale, ak[mt][i + 2] * a.scale, ak[mt][i + 3] * a.scale};
-                const float y[4] = {av[mt][i], av[mt][i + 1], av[mt][i + 2], av[mt][i + 3]};
-                store(dK + o, x);
-                store(dV + o, y);
+            for (int i = 0; i < 16; ++i) {
+                x[i] = ak[mt][i] * a.scale;
+                y[i] = av[mt][i];
+                most = max_nan(max_nan(most, fabsf(x[i])), fabsf(y[i]));
             }
+            store_result(dK + at + 32 * mt, x, h);
+            store_result(dV + at + 32 * mt, y, h);
+        }
     }
     // keys with a sum that is not finite once more, from their own pairs alone
     uint64_t bad = __ballot(!(most < INFINITY));

@@ -588,7 +588,8 @@ static int few_shares(const WindowDims& s)
     const int64_t items = (int64_t)s.bhk * few_groups(s);
     return (int)std::max<int64_t>(1, std::min<int64_t>(256 / items, few_keys(s) / kShareKeys));
 }
-// Few tiles?  The tiled kernels take as long as their longest walk where the chip is not full, the ones here cut it in four but
+// Calls of up to 32 positions: always, for all heads that share keys read them once (1 position of 2047 x 32 heads on 8, 512 keys,
+// d = 128: 1676 -> 707 us).  Otherwise: few tiles?  The tiled kernels take as long as their longest walk where the chip is not full, the ones here cut it in four but
 // take about 1.3 times as long where it is: few, where tiles x average walk < c x longest walk - x.  us, tiled | here, 16 heads,
 // bf16, d = 64: forward N = 1024, W = 256 11.1 | 7.1; 2048 11.6 | 13.0; 2048 dense 40.0 | 26.0; 8192 dense 235 | 241; 4 heads of
 // 8192, W = 2048 42.9 | 35.2; 4096 (16) 51.8 | 53.3.  Backward: N = 1024, W = 256 26.5 | 19.2; 2048 28.3 | 34.2; dense 4096
@@ -605,7 +606,7 @@ static double all_pairs(const WindowDims& s)                 // of one head
 bool window_few(const WindowDims& s)
 {
     const double tiles = (double)s.bh * s.q / 128;
-    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : 230);
+    return s.q <= 32 || tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : 230);
 }
 size_t window_few_ws_bytes(const WindowDims& s)
 {

@@ -116,19 +116,15 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     float most = 0.f;
     if (r0 + m32 < a.q) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+            float o[16];
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                float o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[e] = acc[mt][i + e] * inv;
-                    most = max_nan(most, fabsf(o[e]));
-                }
-                T* to = O + row * D + 32 * mt + result_row(i) + 4 * h;
-                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o[0], o[1]), pack2(o[2], o[3]));
-                else *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+            for (int i = 0; i < 16; ++i) {
+                o[i] = acc[mt][i] * inv;
+                most = max_nan(most, fabsf(o[i]));
             }
+            store_result(O + row * D + 32 * mt, o, h);
+        }
         if (h == 0) lse[row] = empty ? -INFINITY : (ref + fast_log2(L)) * kLn2;
     }
     // A weight of zero does not hide an infinity or a NaN: such rows are done once more, from their own pairs alone

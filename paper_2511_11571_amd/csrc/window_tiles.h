@@ -42,6 +42,24 @@ __device__ __forceinline__ void pack_opnd(Opnd<float>& o, const float* p)
     for (int e = 0; e < 8; ++e) o.v[e] = p[e];
 }
 
+// a result's sixteen channels of column m to the 32 channels of row m that `to` points at.  bf16: the two lanes of a row swap
+// four channels each, so that both write eight neighbouring ones.
+__device__ __forceinline__ void store_result(bf16_t* to, const float (&o)[16], int h)
+{
+#pragma unroll
+    for (int j = 0; j < 16; j += 8) {
+        const auto x = __builtin_amdgcn_permlane32_swap(pack2(o[j], o[j + 1]), pack2(o[j + 4], o[j + 5]), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(pack2(o[j + 2], o[j + 3]), pack2(o[j + 6], o[j + 7]), false, false);
+        *reinterpret_cast<uint4*>(to + 2 * j + 8 * h) = make_uint4(x[0], y[0], x[1], y[1]);
+    }
+}
+__device__ __forceinline__ void store_result(float* to, const float (&o)[16], int h)
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(to + 2 * i + 4 * h) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+}
+
 // sum of sixteen probabilities as they are before they are rounded (in pairs: short chains)
 __device__ __forceinline__ float sum16(const float (&x)[16])
 {
