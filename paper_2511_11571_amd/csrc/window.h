@@ -125,10 +125,10 @@ __device__ __forceinline__ void plain_dq_row(const WindowArgs& a, const T* __res
     for (int c = 0; c < D / 64; ++c) dQ[row * D + lane + 64 * c] = from_f32<T>(lo > t ? 0.f : acc[c] * a.scale);
 }
 
-// dK and dV of key u of key/value slice sk
-template <typename T, int D>
+// dK and dV of key u of key/value slice sk; D of the rows from Dv or (OWN) from O
+template <typename T, int D, bool OWN>
 __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K,
-                                               const T* __restrict__ V, const T* __restrict__ dO,
+                                               const T* __restrict__ V, const T* __restrict__ O, const T* __restrict__ dO,
                                                const float* __restrict__ lse, const float* __restrict__ Dv,
                                                T* __restrict__ dK, T* __restrict__ dV, int sk, int u, int lane)
 {
@@ -144,7 +144,8 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
             float p = 0.f, ds = 0.f;
             if (on) {
                 p = fast_exp2(fmaf(row_dot<T, D>(Q + (base + r) * D, K + key), a.scale * kLog2e, -lse[base + r] * kLog2e));
-                ds = p * (row_dot<T, D>(dO + (base + r) * D, V + key) - Dv[base + r]);
+                const float Dr = OWN ? row_dot<T, D>(dO + (base + r) * D, O + (base + r) * D) : Dv[base + r];
+                ds = p * (row_dot<T, D>(dO + (base + r) * D, V + key) - Dr);
             }
             for (uint64_t left = __ballot(on); left; left &= left - 1) {
                 const int j = __builtin_ctzll(left);
@@ -178,7 +179,11 @@ bool window_few_dkdv(const WindowDims& s);
 hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
                                 const void* dO, const int32_t* first, void* dQ, float* Dv, hipStream_t st);
 hipError_t launch_window_few_dkdv(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
-                                  const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st);
+                                  const int32_t* first, void* dK, void* dV, float* Dv, hipStream_t st);
+// both in one launch
+bool window_few_both(const WindowDims& s);
+hipError_t launch_window_few_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
+                                      const void* dO, const int32_t* first, void* dQ, void* dK, void* dV, float* Dv, hipStream_t st);
 size_t window_backward_ws_bytes(const WindowDims& s);
 hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                                   const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,

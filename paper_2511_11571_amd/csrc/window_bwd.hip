@@ -345,7 +345,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     // keys with a sum that is not finite once more, from their own pairs alone
     uint64_t bad = __ballot(!(most < INFINITY));
     bad = (bad | bad >> 32) & 0xffffffffu;
-    for (; bad; bad &= bad - 1) plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, left.D, dK, dV, skv, ku + __builtin_ctzll(bad), lane);
+    for (; bad; bad &= bad - 1) plain_dkdv_key<T, D, false>(a, Q, K, V, nullptr, dO, lse, left.D, dK, dV, skv, ku + __builtin_ctzll(bad), lane);
 }
 
 // [D of every row][first keys of 32 rows each]
@@ -360,6 +360,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     const WindowArgs a = window_args(s, first);
     float* Dv = static_cast<float*>(ws);
     const bool few_q = window_few_dq(s), few_k = window_few_dkdv(s);
+    if (window_few_both(s)) return launch_window_few_backward(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st);
     int2* lo = first && !few_k ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr;
     hipError_t e;
     if (few_q) {

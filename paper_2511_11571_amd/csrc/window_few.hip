@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int skv, pos;
     if (!schedule(blockIdx.x, a.bhk, groups * shares, skv, pos)) return;
-    const int group = pos / shares, share = pos % shares;
+    const int group = groups - 1 - pos / shares, share = pos % shares;          // (the longest rows first)
     const int rows = a.G * a.q, t0 = a.N - a.q;
     const T* Ks = K + (int64_t)skv * a.rows * D;
     const T* Vs = V + (int64_t)skv * a.rows * D;
@@ -280,19 +280,15 @@ __global__ __launch_bounds__(kFewWaves* kWave) void window_merge_kernel(WindowAr
 
 // dQ: as the forward, the waves' sums added up at the end.  D of every row is left for dK and dV.
 template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
-                                                                            const T* __restrict__ V, const T* __restrict__ O,
-                                                                            const float* __restrict__ lse, const T* __restrict__ dO,
-                                                                            T* __restrict__ dQ, float* __restrict__ Dv, int groups)
+__device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
+                                       const T* __restrict__ O, const float* __restrict__ lse, const T* __restrict__ dO,
+                                       T* __restrict__ dQ, float* __restrict__ Dv, int skv, int group, unsigned char* smem)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
     using KV = Tile<T, D, kFewKeys>;
     constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
-    extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    int skv, group;
-    if (!schedule(blockIdx.x, a.bhk, groups, skv, group)) return;
     const int rows = a.G * a.q, t0 = a.N - a.q;
     const T* Ks = K + (int64_t)skv * a.rows * D;
     const T* Vs = V + (int64_t)skv * a.rows * D;
@@ -405,25 +401,48 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dq_kernel(Wind
     }
 }
 
-// dK and dV of 32 keys: the waves take 32 rows at a time in turn, of all heads that share the keys
-template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(WindowArgs a, const T* __restrict__ Q,
-                                                                              const T* __restrict__ K, const T* __restrict__ V,
-                                                                              const float* __restrict__ lse, const T* __restrict__ dO,
-                                                                              T* __restrict__ dK, T* __restrict__ dV,
-                                                                              const float* __restrict__ Dv, int ktiles)
+// sum over the L neighbouring lanes of a row
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) x += __shfl_xor(x, o, kWave);
+    return x;
+}
+__device__ __forceinline__ float piece_dot(const u32x4_t& x, const u32x4_t& y, bf16_t)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+        s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+    }
+    return s;
+}
+__device__ __forceinline__ float piece_dot(const u32x4_t& x, const u32x4_t& y, float)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fmaf(__uint_as_float(x[i]), __uint_as_float(y[i]), s);
+    return s;
+}
+
+// dK and dV of 32 keys: the waves take 32 rows at a time in turn, of all heads that share the keys.  D of the rows is found
+// in Dv, or (OWN) taken from O on the way, so that nothing has to be done before.
+template <typename T, int D, bool OWN>
+__device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
+                                         const T* __restrict__ O, const float* __restrict__ lse, const T* __restrict__ dO,
+                                         T* __restrict__ dK, T* __restrict__ dV, float* __restrict__ Dv, int skv, int tile,
+                                         unsigned char* smem)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
     using QG = Tile<T, D, 32>;
     constexpr int WAVE_BYTES = 2 * QG::BYTES > 32 * D * 4 ? 2 * QG::BYTES : 32 * D * 4;
-    extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) float stat_z[NW][32], stat_d[NW][32];
     __shared__ __align__(16) int stat_lo[NW][32];
     __shared__ int range[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    int skv, tile;
-    if (!schedule(blockIdx.x, a.bhk, ktiles, skv, tile)) return;
     const int t0 = a.N - a.q, ku = 32 * tile, key = ku + m32;
     Opnd<T> k[STEPS], v[STEPS];
     const int64_t own = ((int64_t)skv * a.rows + min(key, a.N - 1)) * D;
@@ -454,7 +473,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(Wi
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) ak[mt] = av[mt] = f32x16_t{};
     {
-        u32x4_t mq[QG::template pieces<kWave>], mg[QG::template pieces<kWave>];
+        constexpr int P = QG::template pieces<kWave>, LANES = QG::PIECES;
+        u32x4_t mq[P], mg[P], mo[OWN ? P : 1];
         float nz = 0.f, nd = 0.f;
         int nl = 0;
         auto fetch = [&](int i) __attribute__((always_inline)) {
@@ -464,7 +484,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(Wi
             QG::template load<kWave>(mg, dO + base * D, r, a.q - 1, lane);
             const int rr = min(r + m32, a.q - 1);
             nz = -lse[base + rr] * kLog2e;
-            nd = -Dv[base + rr];
+            if constexpr (OWN) QG::template load<kWave>(mo, O + base * D, r, a.q - 1, lane);
+            else nd = -Dv[base + rr];
             nl = window_first(a, s, rr);
         };
         if (wave < total) fetch(wave);
@@ -472,7 +493,16 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(Wi
             const int r = begin + i % per * 32;
             QG::template store<kWave>(mq, mine, lane);
             QG::template store<kWave>(mg, mine + QG::BYTES, lane);
-            if (h == 0) { sz[m32] = nz; sd[m32] = nd; sl[m32] = nl; }
+            if (h == 0) { sz[m32] = nz; sl[m32] = nl; }
+            if constexpr (OWN) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const float x = lanes_sum<LANES>(piece_dot(mo[j], mg[j], T()));
+                    if (lane % LANES == 0) sd[lane / LANES + j * (kWave / LANES)] = -x;
+                }
+            } else if (h == 0) {
+                sd[m32] = nd;
+            }
             const bool late = t0 + r < ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;
             if (i + NW < total) fetch(i + NW);
             f32x16_t S = f32x16_t{}, dP;
@@ -566,7 +596,48 @@ __global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(Wi
     for (uint64_t bad = __ballot(odd); bad;) {
         const int x = __builtin_ctzll(bad) / TPR;
         bad &= ~(((1ull << TPR) - 1) << (x * TPR));
-        plain_dkdv_key<T, D>(a, Q, K, V, dO, lse, Dv, dK, dV, skv, ku + __shfl(c, x * TPR, kWave), lane);
+        const int u = ku + __shfl(c, x * TPR, kWave);
+        plain_dkdv_key<T, D, OWN>(a, Q, K, V, O, dO, lse, Dv, dK, dV, skv, u, lane);
+    }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
+                                                                            const T* __restrict__ V, const T* __restrict__ O,
+                                                                            const float* __restrict__ lse, const T* __restrict__ dO,
+                                                                            T* __restrict__ dQ, float* __restrict__ Dv, int groups)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    int skv, pos;
+    if (schedule(blockIdx.x, a.bhk, groups, skv, pos)) few_dq<T, D>(a, Q, K, V, O, lse, dO, dQ, Dv, skv, groups - 1 - pos, smem);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_dkdv_kernel(WindowArgs a, const T* __restrict__ Q,
+                                                                              const T* __restrict__ K, const T* __restrict__ V,
+                                                                              const float* __restrict__ lse, const T* __restrict__ dO,
+                                                                              T* __restrict__ dK, T* __restrict__ dV,
+                                                                              float* __restrict__ Dv, int ktiles)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    int skv, tile;
+    if (schedule(blockIdx.x, a.bhk, ktiles, skv, tile)) few_dkdv<T, D, false>(a, Q, K, V, nullptr, lse, dO, dK, dV, Dv, skv, tile, smem);
+}
+
+// Both at once, the first `first_k` workgroups (a multiple of eight) for dQ: short calls leave half the chip to either alone
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves* kWave, 1) void window_few_backward_kernel(
+    WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+    const float* __restrict__ lse, const T* __restrict__ dO, T* __restrict__ dQ, T* __restrict__ dK, T* __restrict__ dV,
+    float* __restrict__ Dv, int groups, int grid_q, int first_k, int ktiles)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int b = blockIdx.x;
+    int skv, pos;
+    if (b < first_k) {
+        if (b < grid_q && schedule(b, a.bhk, groups, skv, pos)) few_dq<T, D>(a, Q, K, V, O, lse, dO, dQ, Dv, skv, groups - 1 - pos, smem);
+    } else if (schedule(b - first_k, a.bhk, ktiles, skv, pos)) {
+        few_dkdv<T, D, true>(a, Q, K, V, O, lse, dO, dK, dV, Dv, skv, pos, smem);
     }
 }
 
@@ -653,7 +724,7 @@ static hipError_t few_dq_t(const WindowDims& s, const void* Q, const void* K, co
 }
 template <typename T, int D>
 static hipError_t few_dkdv_t(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
-                             const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st)
+                             const int32_t* first, void* dK, void* dV, float* Dv, hipStream_t st)
 {
     const hipError_t e = window_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>());
     if (e != hipSuccess) return e;
@@ -661,6 +732,20 @@ static hipError_t few_dkdv_t(const WindowDims& s, const void* Q, const void* K, 
     hipLaunchKernelGGL((window_few_dkdv_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(kFewWaves * kWave),
                        (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV,
                        Dv, ktiles);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+static hipError_t few_backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
+                                 const void* dO, const int32_t* first, void* dQ, void* dK, void* dV, float* Dv, hipStream_t st)
+{
+    const hipError_t e = window_lds((const void*)window_few_backward_kernel<T, D>, few_lds<T, D>());
+    if (e != hipSuccess) return e;
+    const int groups = few_groups(s), ktiles = (s.N + 31) / 32;
+    const int grid_q = schedule_grid(s.bhk, groups), first_k = (grid_q + kXcds - 1) / kXcds * kXcds;
+    hipLaunchKernelGGL((window_few_backward_kernel<T, D>), dim3((unsigned)(first_k + schedule_grid(s.bhk, ktiles))),
+                       dim3(kFewWaves * kWave), (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V,
+                       (const T*)O, lse, (const T*)dO, (T*)dQ, (T*)dK, (T*)dV, Dv, groups, grid_q, first_k, ktiles);
     return hipGetLastError();
 }
 
@@ -685,8 +770,27 @@ hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* 
                      : few_dq_t<float, 128>(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);
 }
 
+// One launch for both directions' kernels gains where together they do not fill the chip and loses elsewhere, for dK and dV read O
+// for every 32 keys again.  us, two launches | one, bf16: 16 heads of 100, d = 64 9.9 | 6.2; 16 of 512, W = 256 13.6 | 12.0, d = 128
+// 22.1 | 26.2; 1 of 4096 22.5 | 19.3, of 8192 27.0 | 30.4; 16 on 4 of 512 33.5 | 44.8.  fp32: 4 of 1024, d = 64 35.6 | 25.4, 16 of 512 36.1 | 38.5.
+bool window_few_both(const WindowDims& s)
+{
+    const int64_t groups = (int64_t)s.bhk * (few_groups(s) + (s.N + 31) / 32);
+    return window_few_dq(s) && window_few_dkdv(s) && groups <= (s.D == 64 && s.dtype == MOBA_BF16 && s.G == 1 ? 512 : 256);
+}
+
+hipError_t launch_window_few_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
+                                      const void* dO, const int32_t* first, void* dQ, void* dK, void* dV, float* Dv, hipStream_t st)
+{
+    if (s.dtype == MOBA_BF16)
+        return s.D == 64 ? few_backward_t<bf16_t, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st)
+                         : few_backward_t<bf16_t, 128>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st);
+    return s.D == 64 ? few_backward_t<float, 64>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st)
+                     : few_backward_t<float, 128>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st);
+}
+
 hipError_t launch_window_few_dkdv(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
-                                  const int32_t* first, void* dK, void* dV, const float* Dv, hipStream_t st)
+                                  const int32_t* first, void* dK, void* dV, float* Dv, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
         return s.D == 64 ? few_dkdv_t<bf16_t, 64>(s, Q, K, V, lse, dO, first, dK, dV, Dv, st)

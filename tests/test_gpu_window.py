@@ -56,10 +56,10 @@ def test_forward_and_backward(case, dt, d):
     _check(_shape(b, h, hkv, q, N, d, W, dt), Q, K, V, dO)
 
 
-# enough tiles of queries, or of keys, for the kernels that work tile by tile: both of them; with shared heads; dense; fewer
+# enough tiles of queries, or of keys, for the kernels that work tile by tile: both of them; neither, but each on its own; with shared heads; dense; fewer
 # queries than keys; queries by tiles and keys not (heads that share); the other way round (few queries)
 TILES = [
-    (2, 70, 70, 131, 131, 40), (2, 128, 64, 131, 131, 33), (1, 264, 264, 200, 200, 0), (1, 200, 200, 100, 300, 45),
+    (2, 70, 70, 131, 131, 40), (2, 20, 20, 131, 131, 40), (2, 24, 6, 131, 131, 0), (2, 128, 64, 131, 131, 33), (1, 264, 264, 200, 200, 0), (1, 200, 200, 100, 300, 45),
     (1, 300, 300, 257, 257, 256), (1, 256, 16, 131, 131, 40), (1, 200, 200, 20, 300, 45), (3, 50, 50, 129, 129, 1),
 ]
 
