@@ -128,3 +128,17 @@ def test_a_hybrid_models_layer_runs_together():
     qt, _ = moba.rope(step, Q[:, :, N - 1:].contiguous(), K[:, :, N - 1:].contiguous(), out=(None, cache_k[:, :, N - 1:N]))
     ot, lt = moba.window_forward(moba.WindowShape(b, h, 1, N, d, window=W, dtype=CODE[dt], kv_heads=hkv, kv_rows=N + 8), qt, cache_k, cache_v)
     assert (ot[:, :, 0] - O[:, :, -1]).abs().max() < 1e-5 and (lt[:, :, 0] - lse[:, :, -1]).abs().max() < 1e-5
+
+
+def test_offsets_beyond_32_bits():
+    """2^24 rows of fp32, 8 GB, in place: the last rows as a call on them alone."""
+    n, d = 1 << 24, 128
+    x = torch.empty((1, 1, n, d), device="cuda")
+    x[:, :, :64], x[:, :, -64:] = _draw(7, (1, 1, 64, d), torch.float32), _draw(8, (1, 1, 64, d), torch.float32)
+    ends = x[:, :, :64].clone(), x[:, :, -64:].clone()
+    moba.rope(moba.RopeShape(1, 1, n, d, dtype=binding.F32), x, out=(x, None))
+    for got, a, at in ((x[:, :, :64], ends[0], 0), (x[:, :, -64:], ends[1], n - 64)):
+        want, _ = moba.rope(moba.RopeShape(1, 1, 64, d, dtype=binding.F32, position0=at), a)
+        assert torch.equal(got, want)
+    del x
+    torch.cuda.empty_cache()

@@ -289,3 +289,28 @@ def test_streams_graphs_and_repeats():
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(held, now))
             assert i == 1 or all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 2^24 rows in fp32: the last keys lie 8 GB behind the first, those of the second head 17 GB."""
+    h, N, d, W, q = 2, 1 << 24, 128, 200, 3
+    K, V = (torch.empty((1, h, N, d), device="cuda") for _ in range(2))
+    near = 256
+    g = torch.Generator().manual_seed(17)
+    for t in (K, V):
+        t[:, :, -near:] = torch.randn((1, h, near, d), generator=g).cuda()
+        t[:, :, -near - W:-near] = 0.0
+    Q, dO = (torch.randn((1, h, q, d), generator=g).cuda() for _ in range(2))
+    cut = [t[:, :, -near:].contiguous() for t in (K, V)]
+    sh = _shape(1, h, h, q, N, d, W, torch.float32)
+    O, lse = moba.window_forward(sh, Q, K, V)
+    want = ref.window(Q, *cut, W, None, dO=dO)
+    ref.close(O, want["O"], "O")
+    ref.close(lse, want["lse"], "lse")
+    dQ, dK, dV = moba.window_backward(sh, Q, K, V, O, lse, dO)
+    ref.close(dQ, want["dQ"], "dQ")
+    for name, x in (("dK", dK), ("dV", dV)):
+        ref.close(x[:, :, -near:].contiguous(), want[name], name)
+        assert not x[:, :, :-near].any()                     # keys that no row attends
+    del K, V, dK, dV
+    torch.cuda.empty_cache()
