@@ -99,6 +99,11 @@ __device__ __forceinline__ void plain_forward_row(const WindowArgs& a, const T* 
     if (lane == 0) lse[row] = empty ? -INFINITY : (m + fast_log2(l)) * kLn2;
 }
 
+// Factor of the sums of dQ and of dK.  The gradient with respect to the one logit of a row that attends one key is zero,
+// and dO . v - D only as far as sums in different orders agree.
+__device__ __forceinline__ float dq_factor(const WindowArgs& a, int lo, int t) { return lo < t ? a.scale : 0.f; }
+__device__ __forceinline__ float dk_factor(const WindowArgs& a) { return a.W > 1 ? a.scale : 0.f; }
+
 template <typename T, int D>
 __device__ __forceinline__ void plain_dq_row(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K,
                                              const T* __restrict__ V, const T* __restrict__ dO,
@@ -122,7 +127,7 @@ __device__ __forceinline__ void plain_dq_row(const WindowArgs& a, const T* __res
         add_rows<T, D>(acc, ds, n, lane, [&](int j) { return Ks + (int64_t)(u0 + j) * D; });
     }
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) dQ[row * D + lane + 64 * c] = from_f32<T>(lo > t ? 0.f : acc[c] * a.scale);
+    for (int c = 0; c < D / 64; ++c) dQ[row * D + lane + 64 * c] = from_f32<T>(acc[c] * dq_factor(a, lo, t));
 }
 
 // dK and dV of key u of key/value slice sk; D of the rows from Dv or (OWN) from O
@@ -161,7 +166,7 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
     }
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-        dK[key + lane + 64 * c] = from_f32<T>(ak[c] * a.scale);
+        dK[key + lane + 64 * c] = from_f32<T>(ak[c] * dk_factor(a));
         dV[key + lane + 64 * c] = from_f32<T>(av[c]);
     }
 }

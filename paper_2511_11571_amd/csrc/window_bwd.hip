@@ -137,6 +137,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             if (u0 + KT < end) step(u0 + KT, std::integral_constant<int, 1>());
         }
     }
+    const float factor = dq_factor(a, lo, t);
     float most = 0.f;
     if (mine) {
 #pragma unroll
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
             float o[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                o[i] = acc[mt][i] * a.scale;
+                o[i] = acc[mt][i] * factor;
                 most = max_nan(most, fabsf(o[i]));
             }
             store_result(dQ + row * D + 32 * mt, o, h);
@@ -326,6 +327,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             if (more) arrived(buf ^ 1);
         }
     }
+    const float k_factor = dk_factor(a);
     float most = 0.f;
     if (key < a.N) {
         const int64_t at = ((int64_t)skv * a.rows + key) * D;
@@ -334,7 +336,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             float x[16], y[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[i] = ak[mt][i] * a.scale;
+                x[i] = ak[mt][i] * k_factor;
                 y[i] = av[mt][i];
                 most = max_nan(max_nan(most, fabsf(x[i])), fabsf(y[i]));
             }

@@ -381,13 +381,13 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     if (32 * group + c < rows) {
         cr = (32 * group + c) / a.G;
         cs = skv * a.G + (32 * group + c) % a.G;
-        const bool empty = window_first(a, cs, cr) > t0 + cr;
+        const float factor = dq_factor(a, window_first(a, cs, cr), t0 + cr);
 #pragma unroll
         for (int e = 0; e < CH; e += 8) {
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[i] = empty ? 0.f : o[e + i] * a.scale;
+                x[i] = o[e + i] * factor;
                 odd |= !(fabsf(x[i]) < INFINITY);
             }
             Vec8<T>::store(dQ + ((int64_t)cs * a.q + cr) * D + ch0 + e, x);
@@ -538,6 +538,12 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
                 const int least = key - t0 - r - 4 * h;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) only(j, result_row(j) >= least);
+                // rows that attend their own key alone (sequences of one in a packed batch)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int o = result_row(j) + 4 * h;
+                    ds[j] = sl[o] < t0 + r + o ? ds[j] : 0.f;
+                }
             }
             if (early) {
                 const int most = a.q - 1 - r - 4 * h;
@@ -589,7 +595,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             Vec8<T>::store(to + ((int64_t)skv * a.rows + ku + c) * D + ch0 + e, x);
         }
     };
-    out(ak, dK, a.scale);
+    out(ak, dK, dk_factor(a));
     __syncthreads();
     out(av, dV, 1.f);
     // keys that are not finite once more, from their own pairs alone

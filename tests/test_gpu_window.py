@@ -156,6 +156,23 @@ def test_rows_that_attend_nothing(dt, d, h, hkv, W):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,h,hkv,N,W", [(1, 1, 1, 1, 0), (1, 2, 1, 300, 1), (2, 20, 20, 131, 1), (2, 70, 70, 131, 1), (1, 256, 16, 131, 1)])
+def test_a_single_key_gives_no_gradient_to_its_logit(b, h, hkv, N, W, d, dt):
+    """The softmax of one logit is one: dQ of rows that attend one key is zero, not a rounding (the first row of every
+    sequence is such a row in any window), and so is dK where the window is one key."""
+    Q, K, V, dO = _draw(6, b, h, hkv, N, N, d, dt)
+    _, _, (dQ, dK, dV) = _check(_shape(b, h, hkv, N, N, d, W, dt), Q, K, V, dO)
+    assert not dQ.any() and not dK.any() and dV.any()
+    for first in (None, torch.arange(N, dtype=torch.int32).div(7, rounding_mode="floor").mul(7).expand(b, N).contiguous().cuda()):
+        _, _, (dQ, _, _) = _check(_shape(b, h, hkv, N, N, d, 40, dt), Q, K, V, dO, first)
+        assert not dQ[:, :, 0].any() and (first is None or not dQ[:, :, ::7].any())
+    if h <= 2:                                               # a packed batch of sequences of one
+        _, _, (dQ, dK, _) = _check(_shape(b, h, hkv, N, N, d, 40, dt), Q, K, V, dO, torch.arange(N, dtype=torch.int32).expand(b, N).contiguous().cuda())
+        assert not dQ.any() and not dK.any()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("h,d", [(2, 64), (2, 128), (80, 64), (80, 128)])
 def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(h, d, dt, value):
