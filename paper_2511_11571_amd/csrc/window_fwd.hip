@@ -1,13 +1,21 @@
-// Causal attention to the last W keys: forward.
+// Causal attention to the last W keys: forward, O = softmax(scale Q K^T) V over max(0, t - W + 1, first key) .. t.
 //
-// A workgroup takes a tile of neighbouring queries of one head, a wave 32 of them, and walks the keys that
-// some of them attend in tiles of KT rows through LDS; the next tile is on its way from memory meanwhile.  Scores
-// are computed transposed, S^T = K Q^T, so that a lane holds a query's scores of half the keys and the softmax's
-// maximum and sum cost one exchange of halves; O^T = V^T P^T takes P as it comes out.  Statistics and sums
-// are fp32; P enters its product in the I/O type.
+// A workgroup takes a tile of 128 neighbouring queries of one head, a wave 32 of them, and walks the keys that some of
+// them attend in tiles of KT rows through LDS (two tiles, the next one on its way through registers).  Scores are computed
+// transposed, S^T = K Q^T, so that a lane holds a query's scores of half the keys and the softmax's maximum and sum cost
+// one exchange of halves; O^T = V^T P^T takes P as it comes out.  Statistics and sums are fp32; P enters its product in the
+// I/O type (half a step, 2^-9 of it, which the sum over the keys averages), its sum is taken before that.
 //
 // The reference m of a row's exponents follows its maximum only when that has grown by more than 2^8: P stays
 // below 2^8, and most tiles scale nothing.
+//
+// What bounds it: instruction issue, products and vector units by turns.  A lot of 32 keys x 32 queries at d = 64 is 256 cycles of
+// products and some 400 of exponentials, multiply-adds, maxima, sums and roundings (counters, dense: matrix units 40 %, vector
+// units 70 % busy, LDS 30 %), at d = 128 512 and 450 (44 %, 47 %); the chip's clock goes down to 1.8 GHz meanwhile.  Measured: 16
+// heads on 4 of 16384, d = 128, dense 1.14 ms, 970 TFLOP/s (a library product of 8192^3 1330); 32 of 8192, d = 64, dense 0.38 ms, 725;
+// W = 256, 16 of 32768, d = 64 78 us: 3.4 TB/s of Q, K, V and O, a wave has 9 lots and as much again to begin and end.
+// Slower, us at W = 256, 16 heads of 8192 (25 as it is): 64 queries to a wave 31, two waves to a workgroup 35, eight 26, tiles of 32 keys
+// 26, two lots at once 29, tiles straight into LDS 26; priorities for the products, dense 16384: 1.11 -> 1.21 ms.
 #include "window_tiles.h"
 
 namespace moba {
