@@ -15,9 +15,11 @@
 //
 // What bounds them: issue and latency with two or three waves a SIMD (counters, d = 64 dense: dQ matrix units 52 %, vector units 53 %
 // busy; dK and dV 42 % and 42 %; d = 128, W = 2048: 49 % and 33 %, 43 % and 31 %; LDS 26 to 37 %, no bank conflicts).  Measured, dQ | dK and dV:
-// 32 heads of 8192, d = 64, dense 0.43 | 0.60 ms (960 | 920 TFLOP/s of the products made); 16 heads on 4 of 32768, d = 128, W = 2048
-// 0.80 | 1.13 ms (1000 | 950); 16 of 32768, d = 64, W = 256 102 | 154 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
+// 32 heads of 8192, d = 64, dense 0.43 | 0.59 ms (960 | 930 TFLOP/s of the products made); 16 heads on 4 of 32768, d = 128, W = 2048
+// 0.77 | 1.13 ms (1040 | 950); 16 of 32768, d = 64, W = 256 102 | 150 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
 // queries 640, of 64 (10 registers spilled) 680; two or eight waves to a workgroup 655 and 605, at W = 256 158 and 200.
+// Operands are asked for one product ahead of their use where registers allow: without that dQ 0.44 and 0.81 ms, dK and dV 0.61 and 1.15 ms
+// (d = 64 dense, d = 128); two or three ahead the same, or as many registers spilled as to cost 15 to 60 %.
 #include "window_tiles.h"
 
 namespace moba {
@@ -43,7 +45,7 @@ __global__ __launch_bounds__(256) void window_lo_kernel(WindowArgs a, int2* __re
     if (i < lots && threadIdx.x % 32 == 0) lo[(int64_t)b * lots + i] = make_int2(least, most);
 }
 
-template <typename T, int D, int NW, int KT, int OCC>
+template <typename T, int D, int NW, int KT, int OCC, int QA, int QB>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                               const T* __restrict__ V, const T* __restrict__ O,
                                                               const float* __restrict__ lse, const T* __restrict__ dO,
@@ -93,13 +95,17 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -Dr;
-#pragma unroll
-        for (int e = 0; e < STEPS; ++e) {
-            Opnd<T> k, v;
-            KV::rows(k, kt, row0, e, h, m32);
-            S = mma(k, q[e], S);
-            KV::rows(v, vt, row0, e, h, m32);
-            dP = mma(v, g[e], dP);
+        {
+            Opnd<T> k[QA + 1], v[QA + 1];
+            read_ahead<STEPS, QA>(
+                [&](int e, int i) __attribute__((always_inline)) {
+                    KV::rows(k[i], kt, row0, e, h, m32);
+                    KV::rows(v[i], vt, row0, e, h, m32);
+                },
+                [&](int e, int i) __attribute__((always_inline)) {
+                    S = mma(k[i], q[e], S);
+                    dP = mma(v[i], g[e], dP);
+                });
         }
         float x[16];
 #pragma unroll
@@ -115,14 +121,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
         Opnd<T> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                Opnd<T> k;
-                KV::cols(k, kt, row0 + 16 * j, mt, lane);
-                acc[mt] = mma(k, p[j], acc[mt]);
-            }
+        {
+            Opnd<T> k[QB + 1];
+            read_ahead<2 * MT, QB>(
+                [&](int e, int i) __attribute__((always_inline)) { KV::cols(k[i], kt, row0 + 16 * (e / MT), e % MT, lane); },
+                [&](int e, int i) __attribute__((always_inline)) { acc[e % MT] = mma(k[i], p[e / MT], acc[e % MT]); });
+        }
     };
     if (begin < end) {
         Coming<KV, T, NT, false> next;
@@ -168,7 +172,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     for (; bad; bad &= bad - 1) plain_dq_row<T, D>(a, Q, K, V, dO, lse, Dv, dQ, s, r0 + __builtin_ctzll(bad), lane);
 }
 
-template <typename T, int D, int NW, int QT, int OCC, bool DIRECT>
+// KA, KB: how many products ahead the operands of the first two and of the last two are read
+template <typename T, int D, int NW, int QT, int OCC, bool DIRECT, int KA, int KB>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                                 const T* __restrict__ V, const float* __restrict__ lse,
                                                                 const T* __restrict__ dO, T* __restrict__ dK,
@@ -225,13 +230,17 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             const float4 x = *reinterpret_cast<const float4*>(sd + row0 + result_row(i) + 4 * h);
             dP[i] = x.x; dP[i + 1] = x.y; dP[i + 2] = x.z; dP[i + 3] = x.w;
         }
-#pragma unroll
-        for (int e = 0; e < STEPS; ++e) {
-            Opnd<T> x;
-            QG::rows(x, qt, row0, e, h, m32);
-            S = mma(x, k[e], S);
-            QG::rows(x, gt, row0, e, h, m32);
-            dP = mma(x, v[e], dP);
+        {
+            Opnd<T> x[KA + 1], y[KA + 1];
+            read_ahead<STEPS, KA>(
+                [&](int e, int i) __attribute__((always_inline)) {
+                    QG::rows(x[i], qt, row0, e, h, m32);
+                    QG::rows(y[i], gt, row0, e, h, m32);
+                },
+                [&](int e, int i) __attribute__((always_inline)) {
+                    S = mma(x[i], k[e], S);
+                    dP = mma(y[i], v[e], dP);
+                });
         }
         float p[16], ds[16];
 #pragma unroll
@@ -270,19 +279,23 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
                 }
             }
         }
+        Opnd<T> pp[2], pd[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            Opnd<T> pp, pd;
-            pack_opnd(pp, p + 8 * j);
-            pack_opnd(pd, ds + 8 * j);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                Opnd<T> x;
-                QG::cols(x, gt, row0 + 16 * j, mt, lane);
-                av[mt] = mma(x, pp, av[mt]);
-                QG::cols(x, qt, row0 + 16 * j, mt, lane);
-                ak[mt] = mma(x, pd, ak[mt]);
-            }
+            pack_opnd(pp[j], p + 8 * j);
+            pack_opnd(pd[j], ds + 8 * j);
+        }
+        {
+            Opnd<T> x[KB + 1], y[KB + 1];
+            read_ahead<2 * MT, KB>(
+                [&](int e, int i) __attribute__((always_inline)) {
+                    QG::cols(x[i], gt, row0 + 16 * (e / MT), e % MT, lane);
+                    QG::cols(y[i], qt, row0 + 16 * (e / MT), e % MT, lane);
+                },
+                [&](int e, int i) __attribute__((always_inline)) {
+                    av[e % MT] = mma(x[i], pp[e / MT], av[e % MT]);
+                    ak[e % MT] = mma(y[i], pd[e / MT], ak[e % MT]);
+                });
         }
     };
     float nz = 0.f, nd = 0.f;
@@ -365,7 +378,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
 size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
-template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT>
+template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT, int KA, int KB, int QA, int QB>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                              const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,
                              void* ws, hipStream_t st)
@@ -381,7 +394,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
         if (e != hipSuccess) return e;
     } else {
         constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
-        auto* kernel = window_dq_kernel<T, D, NW, KT, OCCQ>;
+        auto* kernel = window_dq_kernel<T, D, NW, KT, OCCQ, QA, QB>;
         e = window_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
         const int tiles = (s.q + 32 * NW - 1) / (32 * NW);
@@ -398,7 +411,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
         if (e != hipSuccess) return e;
     }
     constexpr size_t lds = 4 * Tile<T, D, QT>::BYTES;
-    auto* kernel = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT>;
+    auto* kernel = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT, KA, KB>;
     e = window_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     const int tiles = (s.N + 32 * NW - 1) / (32 * NW);
@@ -412,10 +425,10 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
                                   void* ws, hipStream_t st)
 {
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2, false>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 2, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                     : backward_t<float, 128, 4, 32, 32, 1, 1, true>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+        return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2, false, 1, 1, 0, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                         : backward_t<bf16_t, 128, 4, 32, 32, 2, 2, true, 0, 1, 1, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2, true, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                     : backward_t<float, 128, 4, 32, 32, 1, 1, true, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 
 }  // namespace moba

@@ -12,15 +12,15 @@
 // What bounds it: instruction issue, products and vector units by turns.  A lot of 32 keys x 32 queries at d = 64 is 256 cycles of
 // products and some 400 of exponentials, multiply-adds, maxima, sums and roundings (counters, dense: matrix units 40 %, vector
 // units 70 % busy, LDS 30 %), at d = 128 512 and 450 (44 %, 47 %); the chip's clock goes down to 1.8 GHz meanwhile.  Measured: 16
-// heads on 4 of 16384, d = 128, dense 1.14 ms, 970 TFLOP/s (a library product of 8192^3 1330); 32 of 8192, d = 64, dense 0.38 ms, 725;
+// heads on 4 of 16384, d = 128, dense 1.13 ms, 970 TFLOP/s (a library product of 8192^3 1330); 32 of 8192, d = 64, dense 0.38 ms, 725;
 // W = 256, 16 of 32768, d = 64 78 us: 3.4 TB/s of Q, K, V and O, a wave has 9 lots and as much again to begin and end.
 // Slower, us at W = 256, 16 heads of 8192 (25 as it is): 64 queries to a wave 31, two waves to a workgroup 35, eight 26, tiles of 32 keys
-// 26, two lots at once 29, tiles straight into LDS 26; priorities for the products, dense 16384: 1.11 -> 1.21 ms.
+// 26, two lots at once 29, tiles straight into LDS 26; priorities for the products, dense 16384: 1.11 -> 1.21 ms; without operands read ahead of their products 1 to 2 % at each size.
 #include "window_tiles.h"
 
 namespace moba {
 
-template <typename T, int D, int NW, int KT, int OCC>
+template <typename T, int D, int NW, int KT, int OCC, int KA, int VA>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
                                                                    const T* __restrict__ K, const T* __restrict__ V,
                                                                    T* __restrict__ O, float* __restrict__ lse, int ntiles)
@@ -52,11 +52,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
     auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{};
-#pragma unroll
-        for (int e = 0; e < STEPS; ++e) {
-            Opnd<T> x;
-            KV::rows(x, kt, row0, e, h, m32);
-            S = mma(x, q[e], S);
+        {
+            Opnd<T> k[KA + 1];
+            read_ahead<STEPS, KA>([&](int e, int i) __attribute__((always_inline)) { KV::rows(k[i], kt, row0, e, h, m32); },
+                                  [&](int e, int i) __attribute__((always_inline)) { S = mma(k[i], q[e], S); });
         }
         float x[16];
 #pragma unroll
@@ -86,14 +85,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
         Opnd<T> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                Opnd<T> v;
-                KV::cols(v, vt, row0 + 16 * j, mt, lane);
-                acc[mt] = mma(v, p[j], acc[mt]);
-            }
+        {
+            Opnd<T> v[VA + 1];
+            read_ahead<2 * MT, VA>(
+                [&](int e, int i) __attribute__((always_inline)) { KV::cols(v[i], vt, row0 + 16 * (e / MT), e % MT, lane); },
+                [&](int e, int i) __attribute__((always_inline)) { acc[e % MT] = mma(v[i], p[e / MT], acc[e % MT]); });
+        }
     };
     if (begin < end) {
         Coming<KV, T, NT, false> next;
@@ -143,11 +140,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 
 size_t window_forward_ws_bytes(const WindowDims& s) { return window_few(s) ? window_few_ws_bytes(s) : 0; }
 
-template <typename T, int D, int NW, int KT, int OCC>
+template <typename T, int D, int NW, int KT, int OCC, int KA, int VA>
 static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                           void* O, float* lse, hipStream_t st)
 {
-    auto* kernel = window_forward_kernel<T, D, NW, KT, OCC>;
+    auto* kernel = window_forward_kernel<T, D, NW, KT, OCC, KA, VA>;
     constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
     const hipError_t e = window_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
@@ -163,10 +160,10 @@ hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void*
 {
     if (window_few(s)) return launch_window_few(s, Q, K, V, first, O, lse, ws, st);
     if (s.dtype == MOBA_BF16)
-        return s.D == 64 ? tiles_t<bf16_t, 64, 4, 64, 4>(s, Q, K, V, first, O, lse, st)
-                         : tiles_t<bf16_t, 128, 4, 64, 2>(s, Q, K, V, first, O, lse, st);
-    return s.D == 64 ? tiles_t<float, 64, 4, 32, 3>(s, Q, K, V, first, O, lse, st)
-                     : tiles_t<float, 128, 4, 32, 2>(s, Q, K, V, first, O, lse, st);
+        return s.D == 64 ? tiles_t<bf16_t, 64, 4, 64, 4, 0, 1>(s, Q, K, V, first, O, lse, st)
+                         : tiles_t<bf16_t, 128, 4, 64, 2, 2, 3>(s, Q, K, V, first, O, lse, st);
+    return s.D == 64 ? tiles_t<float, 64, 4, 32, 3, 0, 0>(s, Q, K, V, first, O, lse, st)
+                     : tiles_t<float, 128, 4, 32, 2, 0, 0>(s, Q, K, V, first, O, lse, st);
 }
 
 }  // namespace moba

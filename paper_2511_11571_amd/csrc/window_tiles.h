@@ -121,8 +121,8 @@ struct Tile {
             const int row = tid / PIECES + i * (NT / PIECES);
             const char* at = reinterpret_cast<const char*>(slice) + (int64_t)min(first + row, last) * RB + 16 * ((tid % PIECES) ^ place(row));
             const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
-            // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory", "m0");
+            // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS.  It keeps nothing in m0.)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory");
         }
     }
 
@@ -192,6 +192,21 @@ struct Coming {
         }
     }
 };
+
+// use(i, slot) for i = 0 .. N - 1, what load(i + AHEAD, slot) asks for on its way meanwhile (AHEAD + 1 slots).  Left to itself the
+// compiler reads an operand, waits and multiplies.
+template <int N, int AHEAD, typename L, typename U>
+__device__ __forceinline__ void read_ahead(L load, U use)
+{
+#pragma unroll
+    for (int i = 0; i < AHEAD && i < N; ++i) load(i, i % (AHEAD + 1));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + AHEAD < N) load(i + AHEAD, (i + AHEAD) % (AHEAD + 1));
+        if (AHEAD > 0) __builtin_amdgcn_sched_barrier(0);
+        use(i, i % (AHEAD + 1));
+    }
+}
 
 __device__ __forceinline__ int wave_min_i(int x)
 {
