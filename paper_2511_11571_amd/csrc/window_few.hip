@@ -507,7 +507,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             } else if (h == 0) {
                 sd[m32] = nd;
             }
-            const bool late = t0 + r < ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;
+            const bool late = t0 + r <= ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;   // late: a row's own key is among them
             if (i + NW < total) fetch(i + NW);
             f32x16_t S = f32x16_t{}, dP;
 #pragma unroll

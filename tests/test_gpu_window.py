@@ -173,6 +173,17 @@ def test_a_single_key_gives_no_gradient_to_its_logit(b, h, hkv, N, W, d, dt):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q,N", [(33, 64), (32, 63), (40, 111), (17, 33), (5, 5)])
+def test_sequences_of_one_at_the_end_of_a_cache(q, N, d, dt):
+    """As above, with the rows' positions shifted against the tiles of the keys."""
+    Q, K, V, dO = _draw(7, 1, 2, 2, q, N, d, dt)
+    first = torch.arange(N - q, N, dtype=torch.int32).view(1, q).cuda()
+    _, _, (dQ, dK, _) = _check(_shape(1, 2, 2, q, N, d, 0, dt), Q, K, V, dO, first)
+    assert not dQ.any() and not dK.any()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("h,d", [(2, 64), (2, 128), (80, 64), (80, 128)])
 def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(h, d, dt, value):
