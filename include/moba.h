@@ -337,6 +337,8 @@ typedef struct moba_window_shape {
  *   O          out  [b,heads,q_len,d] dtype;   lse out [b,heads,q_len] fp32
  *   ws              at least the bytes that moba_window_workspace names (may be NULL where that is 0), of
  *                   any content, used by one call at a time
+ * No output, ws among them, may overlap an input or another output, nor may it in the backward (MOBA_EINVAL
+ * where two start at the same address).
  * Tensors of dtype and ws start on 16-byte boundaries, lse and first_key on 4-byte ones (else MOBA_EINVAL).  kv_len <= kv_rows <= 2^24,
  * q_len <= kv_len, batch * heads <= 65535; otherwise MOBA_EINVAL or, for the two limits,
  * MOBA_EUNSUPPORTED.  Results are the same in every run.
@@ -352,7 +354,6 @@ int moba_window_forward(const moba_window_shape* shape, const void* Q, const voi
  *   dQ         out  [b,heads,q_len,d] dtype
  *   dK, dV     out  [b,kv,kv_rows,d] dtype, rows below kv_len, summed over the query heads that share the
  *                   head; keys that no row attends get zeros
- * No output may overlap an input or another output.
  */
 int moba_window_backward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,
                          const void* O, const float* lse, const void* dO, const int32_t* first_key,
@@ -395,7 +396,7 @@ typedef struct moba_rope_shape {
 /*
  * Turns Q [b,heads,q_rows,d] and, unless K is NULL, K [b,kv,k_rows,d]: rows 0 .. seqlen - 1 of every
  * slice, to the same rows of Q_out and K_out.  An output may be its input (then with the same rows per
- * slice); otherwise no output overlaps an input or the other output.
+ * slice); otherwise no output overlaps an input or the other output (MOBA_EINVAL where they are the same).
  *   positions  in   [b,seqlen] int32, or NULL
  * moba_rope_backward maps gradients with respect to Q_out and K_out to those with respect to Q and K (the
  * turn backwards, the same amplitude).  head_dim 64 or 128.  Pointers to tensors on 16-byte boundaries

@@ -199,6 +199,19 @@ bool aligned(uintptr_t to, std::initializer_list<const void*> ps)
     return all % to == 0;
 }
 
+// no output is an input or another output
+bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins)
+{
+    for (auto o = outs.begin(); o != outs.end(); ++o) {
+        if (!*o) continue;
+        for (auto p = outs.begin(); p != o; ++p)
+            if (*p == *o) return false;
+        for (const void* p : ins)
+            if (p == *o) return false;
+    }
+    return true;
+}
+
 int make_window_dims(const moba_window_shape* sh, WindowDims& d)
 {
     if (!sh) return MOBA_EINVAL;
@@ -290,6 +303,7 @@ int run_rope(const moba_rope_shape* shape, float sign, const void* Q, const void
     if (st != MOBA_OK) return st;
     if (!Q || !Qo || !K != !Ko) return MOBA_EINVAL;
     if ((Q == Qo && a.xrows[0] != a.yrows[0]) || (K && K == Ko && a.xrows[1] != a.yrows[1])) return MOBA_EINVAL;
+    if (!apart({Qo, Ko}, {positions}) || K == Qo || Q == Ko) return MOBA_EINVAL;
     if (!aligned(a.dtype == MOBA_BF16 ? 2 : 4, {Q, K, Qo, Ko}) || !aligned(4, {positions})) return MOBA_EINVAL;
     a.x[0] = Q;
     a.y[0] = Qo;
@@ -618,6 +632,7 @@ int moba_window_forward(const moba_window_shape* shape, const void* Q, const voi
     if (!aligned(16, {Q, K, V, O, ws}) || !aligned(4, {first_key, lse})) return MOBA_EINVAL;
     const size_t need = window_forward_ws_bytes(d);
     if (need > 0 && (!ws || ws_bytes < need)) return MOBA_EWORKSPACE;
+    if (!apart({O, lse, ws}, {Q, K, V, first_key})) return MOBA_EINVAL;
     return hip_status(launch_window_forward(d, Q, K, V, first_key, O, lse, ws, (hipStream_t)stream));
 }
 
@@ -631,6 +646,7 @@ int moba_window_backward(const moba_window_shape* shape, const void* Q, const vo
     if (!Q || !K || !V || !O || !lse || !dO || !dQ || !dK || !dV) return MOBA_EINVAL;
     if (!aligned(16, {Q, K, V, O, dO, dQ, dK, dV, ws}) || !aligned(4, {first_key, lse})) return MOBA_EINVAL;
     if (!ws || ws_bytes < window_backward_ws_bytes(d)) return MOBA_EWORKSPACE;
+    if (!apart({dQ, dK, dV, ws}, {Q, K, V, O, lse, dO, first_key})) return MOBA_EINVAL;
     return hip_status(launch_window_backward(d, Q, K, V, O, lse, dO, first_key, dQ, dK, dV, ws, (hipStream_t)stream));
 }
 

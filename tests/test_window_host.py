@@ -76,6 +76,23 @@ def test_window_pointers_and_workspaces_that_are_refused(lib):
     assert len(ok) == 8
 
 
+def test_outputs_that_are_inputs_or_one_another_are_refused(lib):
+    sh = _window(batch=1, q_len=1, kv_len=200000, window=0)   # (a call that takes a workspace)
+    big = ctypes.c_size_t(1 << 40)
+    at = [P * (i + 1) for i in range(11)]
+    for outs, n, f in (((4, 5, 6), 7, lib.moba_window_forward), ((7, 8, 9, 10), 11, lib.moba_window_backward)):
+        for o in outs:
+            for i in range(n):
+                if i != o:
+                    a = at[:n]
+                    a[o] = a[i]
+                    assert f(ctypes.byref(sh.c()), *[_ptr(x) for x in a], big, None) == EINVAL, (o, i)
+    sh = ctypes.byref(_rope().c())
+    for f in (lib.moba_rope, lib.moba_rope_backward):
+        for q, k, qo, ko in ((1, 2, 3, 3), (1, 2, 2, 3), (1, 2, 2, 1), (1, 2, 3, 1), (1, 1, 1, 2), (1, 2, 5, 2), (1, 2, 1, 5)):
+            assert f(sh, _ptr(q * P), _ptr(k * P), _ptr(5 * P), _ptr(qo * P), _ptr(ko * P), None) == EINVAL
+
+
 def _rope(**kw):
     base = dict(batch=2, heads=4, seqlen=30, head_dim=64, kv_heads=2)
     base.update(kw)
