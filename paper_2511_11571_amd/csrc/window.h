@@ -42,7 +42,8 @@ __device__ __forceinline__ int window_first(const WindowArgs& a, int s, int r)
 // ---- one row, or one key, by a wave: plain loops over its pairs alone ---------------------------
 // They touch nothing but the row's own pairs, so what stands elsewhere cannot reach the result: the tiled
 // kernels, where a weight of zero meets every key and value of a tile, come here with rows and keys
-// whose sums are not finite.
+// whose sums are not finite.  A sum that is NaN stays so: once every channel's is, the loops end, so that a call whose
+// inputs are NaN throughout does not do all its pairs twice.
 template <typename T, int D>
 __device__ __forceinline__ float row_dot(const T* __restrict__ x, const T* __restrict__ y)
 {
@@ -70,6 +71,16 @@ __device__ __forceinline__ void add_rows(float (&acc)[D / 64], float w, int n, i
     }
 }
 
+// every channel's sum is NaN
+template <int C>
+__device__ __forceinline__ bool all_nan(const float (&acc)[C])
+{
+    bool x = true;
+#pragma unroll
+    for (int c = 0; c < C; ++c) x = x && acc[c] != acc[c];
+    return __ballot(!x) == 0;
+}
+
 template <typename T, int D>
 __device__ __forceinline__ void plain_forward_row(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K,
                                                   const T* __restrict__ V, T* __restrict__ O, float* __restrict__ lse,
@@ -92,6 +103,7 @@ __device__ __forceinline__ void plain_forward_row(const WindowArgs& a, const T* 
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) acc[c] *= alpha;
         add_rows<T, D>(acc, p, n, lane, [&](int j) { return Vs + (int64_t)(u0 + j) * D; });
+        if (l != l) break;                                   // (the same in every lane)
     }
     const bool empty = lo > t;
 #pragma unroll
@@ -125,6 +137,7 @@ __device__ __forceinline__ void plain_dq_row(const WindowArgs& a, const T* __res
             ds = p * (row_dot<T, D>(dO + row * D, Vs + key) - Dr);
         }
         add_rows<T, D>(acc, ds, n, lane, [&](int j) { return Ks + (int64_t)(u0 + j) * D; });
+        if (all_nan(acc)) break;
     }
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) dQ[row * D + lane + 64 * c] = from_f32<T>(acc[c] * dq_factor(a, lo, t));
@@ -143,7 +156,7 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
     for (int g = 0; g < a.G; ++g) {
         const int s = sk * a.G + g;
         const int64_t base = (int64_t)s * a.q;
-        for (int r0 = r_lo; r0 < r_hi; r0 += kWave) {
+        for (int r0 = r_lo; r0 < r_hi && !(all_nan(ak) && all_nan(av)); r0 += kWave) {
             const int r = r0 + lane;
             const bool on = r < r_hi && window_first(a, s, r) <= u;
             float p = 0.f, ds = 0.f;

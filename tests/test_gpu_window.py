@@ -220,6 +220,38 @@ def test_a_bad_value_reaches_the_rows_that_attend_it_and_no_other(h, d, dt, valu
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("h,q,N,W", [(2, 300, 300, 100), (80, 300, 300, 100), (2, 3, 3000, 0), (130, 140, 140, 0)])
+def test_nan_throughout(h, q, N, W, d, dt):
+    """What a diverged model hands over: every row's own pairs are NaN, and so is everything that has some.  A sequence
+    that starts at key 70 has none of them where the NaN end there."""
+    Q, K, V, dO = _draw(14, 1, h, h, q, N, d, dt)
+    sh = _shape(1, h, h, q, N, d, W, dt)
+    nan = torch.full_like(K, float("nan"))
+    O, lse = moba.window_forward(sh, Q, nan, V)
+    assert torch.isnan(O).all() and torch.isnan(lse).all()
+    dQ, dK, dV = moba.window_backward(sh, Q, nan, V, O, lse, dO)
+    t = torch.arange(N - q, N)
+    single = (t == 0) | (W == 1)
+    assert torch.isnan(dQ[:, :, ~single]).all()
+    seen = torch.from_numpy(ref.seen(q, N, W, None, 1)[0].any(0).copy())
+    assert torch.isnan(dV[:, :, seen]).all() and torch.isnan(dK[:, :, seen]).all()
+    assert not dV[:, :, ~seen].any() and not dK[:, :, ~seen].any()
+    if q == N:
+        start = torch.full((1, q), 70, dtype=torch.int32)
+        start[:, :70] = 0
+        K2 = K.clone()
+        K2[:, :, :70] = float("nan")
+        first = start.cuda()
+        O, lse = moba.window_forward(sh, Q, K2, V, first_key=first)
+        grads = moba.window_backward(sh, Q, K2, V, O, lse, dO, first_key=first)
+        want = ref.window(Q, K, V, W, first, dO=dO)
+        for name, x in zip(("O", "lse", "dQ", "dK", "dV"), (O, lse) + grads):
+            ref.close(x[:, :, 70:], tuple(w[:, :, 70:] for w in want[name]), name)
+            assert torch.isnan(x[:, :, 1:70]).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("scale", [0.3, 1e-4])
 @pytest.mark.parametrize("h,W", [(2, 128), (70, 50)])
 def test_scales_and_large_logits(h, W, dt, scale):
