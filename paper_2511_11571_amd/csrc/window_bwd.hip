@@ -13,13 +13,13 @@
 // the last two it would be 2.4e-3: dS in two halves would cost two products of seven, D from the probabilities a product more
 // for dQ (a quarter of its time) and at d = 128 more registers than two waves have.
 //
-// What bounds them: issue and latency with two or three waves a SIMD (counters, d = 64 dense: dQ matrix units 52 %, vector units 53 %
-// busy; dK and dV 42 % and 42 %; d = 128, W = 2048: 49 % and 33 %, 43 % and 31 %; LDS 26 to 37 %, no bank conflicts).  Measured, dQ | dK and dV:
-// 32 heads of 8192, d = 64, dense 0.43 | 0.59 ms (960 | 930 TFLOP/s of the products made); 16 heads on 4 of 32768, d = 128, W = 2048
-// 0.77 | 1.13 ms (1040 | 950); 16 of 32768, d = 64, W = 256 102 | 150 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
+// What bounds them: issue and latency with two or three waves a SIMD (counters, d = 64 dense: dQ matrix units 51 %, vector units 53 %
+// busy; dK and dV 43 % and 43 %; d = 128, W = 2048: 53 % and 36 %, 45 % and 33 %; LDS 28 to 38 %, no bank conflicts).  Measured, dQ | dK and dV:
+// 32 heads of 8192, d = 64, dense 0.44 | 0.60 ms (940 | 920 TFLOP/s of the products made); 16 heads on 4 of 32768, d = 128, W = 2048
+// 0.78 | 1.15 ms (1030 | 930); 16 of 32768, d = 64, W = 256 102 | 150 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
 // queries 640, of 64 (10 registers spilled) 680; two or eight waves to a workgroup 655 and 605, at W = 256 158 and 200.
-// Operands are asked for one product ahead of their use where registers allow: without that dQ 0.44 and 0.81 ms, dK and dV 0.61 and 1.15 ms
-// (d = 64 dense, d = 128); two or three ahead the same, or as many registers spilled as to cost 15 to 60 %.
+// Operands are asked for one product ahead of their use where registers allow, which gains 1 to 2 %, for dQ at d = 128 5 %; two or three ahead
+// the same, or as many registers spilled as to cost 15 to 60 %.
 #include "window_tiles.h"
 
 namespace moba {
