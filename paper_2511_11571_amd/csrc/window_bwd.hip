@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void window_lo_kernel(WindowArgs a, int2* __re
     if (i < lots && threadIdx.x % 32 == 0) lo[(int64_t)b * lots + i] = make_int2(least, most);
 }
 
-template <typename T, int D, int NW, int KT, int OCC, int QA, int QB>
+template <typename M, int D, int NW, int KT, int OCC, int QA, int QB, typename T = in_memory_t<M>>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                               const T* __restrict__ V, const T* __restrict__ O,
                                                               const float* __restrict__ lse, const T* __restrict__ dO,
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
                                                               int2* __restrict__ lo_out, int ntiles)
 {
     constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
-    using KV = Tile<T, D, KT>;
+    using KV = Tile<M, D, KT>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int wg_lo[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     const int t0 = a.N - a.q, r0 = tile * QT + wave * 32;
     const int r = min(r0 + m32, a.q - 1), t = t0 + r, lo = window_first(a, s, r);
     const int64_t row = (int64_t)s * a.q + r;
-    Opnd<T> q[STEPS], g[STEPS];
+    Opnd<M> q[STEPS], g[STEPS];
     float Dr = 0.f;
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -Dr;
         {
-            Opnd<T> k[QA + 1], v[QA + 1];
+            Opnd<M> k[QA + 1], v[QA + 1];
             read_ahead<STEPS, QA>(
                 [&](int e, int i) __attribute__((always_inline)) {
                     KV::rows(k[i], kt, row0, e, h, m32);
@@ -118,11 +118,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : 0.f;
         }
-        Opnd<T> p[2];
+        Opnd<M> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
         {
-            Opnd<T> k[QB + 1];
+            Opnd<M> k[QB + 1];
             read_ahead<2 * MT, QB>(
                 [&](int e, int i) __attribute__((always_inline)) { KV::cols(k[i], kt, row0 + 16 * (e / MT), e % MT, lane); },
                 [&](int e, int i) __attribute__((always_inline)) { acc[e % MT] = mma(k[i], p[e / MT], acc[e % MT]); });
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
 }
 
 // KA, KB: how many products ahead the operands of the first two and of the last two are read
-template <typename T, int D, int NW, int QT, int OCC, bool DIRECT, int KA, int KB>
+template <typename M, int D, int NW, int QT, int OCC, bool DIRECT, int KA, int KB, typename T = in_memory_t<M>>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs a, const T* __restrict__ Q, const T* __restrict__ K,
                                                                 const T* __restrict__ V, const float* __restrict__ lse,
                                                                 const T* __restrict__ dO, T* __restrict__ dK,
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 {
     constexpr int NT = NW * kWave, KTILE = 32 * NW, STEPS = D / 16, MT = D / 32;
     static_assert(QT <= kWave, "a lane per row of a tile");
-    using QG = Tile<T, D, QT>;
+    using QG = Tile<M, D, QT>;
     extern __shared__ __align__(16) unsigned char smem[];    // Q, dO | Q, dO
     __shared__ __align__(16) float stat_z[2][QT], stat_d[2][QT];             // -lse (log2 units), -D
     __shared__ __align__(16) int stat_lo[2][QT];
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     int skv, tile;
     if (!schedule(blockIdx.x, a.bhk, ntiles, skv, tile)) return;             // (the first keys have the most queries)
     const int t0 = a.N - a.q, k0 = tile * KTILE, ku = k0 + wave * 32, key = ku + m32;
-    Opnd<T> k[STEPS], v[STEPS];
+    Opnd<M> k[STEPS], v[STEPS];
     {
         const int64_t at = ((int64_t)skv * a.rows + min(key, a.N - 1)) * D;  // (keys past the end: the last one, not stored)
 #pragma unroll
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             dP[i] = x.x; dP[i + 1] = x.y; dP[i + 2] = x.z; dP[i + 3] = x.w;
         }
         {
-            Opnd<T> x[KA + 1], y[KA + 1];
+            Opnd<M> x[KA + 1], y[KA + 1];
             read_ahead<STEPS, KA>(
                 [&](int e, int i) __attribute__((always_inline)) {
                     QG::rows(x[i], qt, row0, e, h, m32);
@@ -279,14 +279,14 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
                 }
             }
         }
-        Opnd<T> pp[2], pd[2];
+        Opnd<M> pp[2], pd[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             pack_opnd(pp[j], p + 8 * j);
             pack_opnd(pd[j], ds + 8 * j);
         }
         {
-            Opnd<T> x[KB + 1], y[KB + 1];
+            Opnd<M> x[KB + 1], y[KB + 1];
             read_ahead<2 * MT, KB>(
                 [&](int e, int i) __attribute__((always_inline)) {
                     QG::cols(x[i], gt, row0 + 16 * (e / MT), e % MT, lane);
@@ -378,11 +378,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
 size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
-template <typename T, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT, int KA, int KB, int QA, int QB>
+template <typename M, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT, int KA, int KB, int QA, int QB>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
                              const float* lse, const void* dO, const int32_t* first, void* dQ, void* dK, void* dV,
                              void* ws, hipStream_t st)
 {
+    using T = in_memory_t<M>;
     const WindowArgs a = window_args(s, first);
     float* Dv = static_cast<float*>(ws);
     const bool few_q = window_few_dq(s), few_k = window_few_dkdv(s);
@@ -393,8 +394,8 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
         e = launch_window_few_dq(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);
         if (e != hipSuccess) return e;
     } else {
-        constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
-        auto* kernel = window_dq_kernel<T, D, NW, KT, OCCQ, QA, QB>;
+        constexpr size_t lds = 4 * Tile<M, D, KT>::BYTES;
+        auto* kernel = window_dq_kernel<M, D, NW, KT, OCCQ, QA, QB>;
         e = window_lds((const void*)kernel, lds);
         if (e != hipSuccess) return e;
         const int tiles = (s.q + 32 * NW - 1) / (32 * NW);
@@ -410,8 +411,8 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    constexpr size_t lds = 4 * Tile<T, D, QT>::BYTES;
-    auto* kernel = window_dkdv_kernel<T, D, NW, QT, OCCK, DIRECT, KA, KB>;
+    constexpr size_t lds = 4 * Tile<M, D, QT>::BYTES;
+    auto* kernel = window_dkdv_kernel<M, D, NW, QT, OCCK, DIRECT, KA, KB>;
     e = window_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     const int tiles = (s.N + 32 * NW - 1) / (32 * NW);
@@ -427,8 +428,8 @@ hipError_t launch_window_backward(const WindowDims& s, const void* Q, const void
     if (s.dtype == MOBA_BF16)
         return s.D == 64 ? backward_t<bf16_t, 64, 4, 64, 64, 3, 2, false, 1, 1, 0, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
                          : backward_t<bf16_t, 128, 4, 32, 32, 2, 2, true, 0, 1, 1, 1>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
-    return s.D == 64 ? backward_t<float, 64, 4, 32, 32, 2, 2, true, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
-                     : backward_t<float, 128, 4, 32, 32, 1, 1, true, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
+    return s.D == 64 ? backward_t<Split, 64, 4, 32, 32, 2, 2, false, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st)
+                     : backward_t<Split, 128, 4, 32, 32, 1, 1, false, 0, 0, 0, 0>(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, ws, st);
 }
 
 }  // namespace moba

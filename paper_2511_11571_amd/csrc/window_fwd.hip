@@ -22,13 +22,13 @@
 
 namespace moba {
 
-template <typename T, int D, int NW, int KT, int OCC, int KA, int VA>
+template <typename M, int D, int NW, int KT, int OCC, int KA, int VA, typename T = in_memory_t<M>>
 __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowArgs a, const T* __restrict__ Q,
                                                                    const T* __restrict__ K, const T* __restrict__ V,
                                                                    T* __restrict__ O, float* __restrict__ lse, int ntiles)
 {
     constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
-    using KV = Tile<T, D, KT>;
+    using KV = Tile<M, D, KT>;
     extern __shared__ __align__(16) unsigned char smem[];    // K, V | K, V
     __shared__ int wg_lo[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     const int t0 = a.N - a.q, r0 = tile * QT + wave * 32;
     const int r = min(r0 + m32, a.q - 1), t = t0 + r, lo = window_first(a, s, r);            // (rows past the end: the last one again, not stored)
     const int64_t row = (int64_t)s * a.q + r;
-    Opnd<T> q[STEPS];
+    Opnd<M> q[STEPS];
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) load_opnd(q[e], Q + row * D + 16 * e + 8 * h);
     const WaveKeys k = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_lo);
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     auto keys32 = [&](const unsigned char* kt, const unsigned char* vt, int row0, int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{};
         {
-            Opnd<T> k[KA + 1];
+            Opnd<M> k[KA + 1];
             read_ahead<STEPS, KA>([&](int e, int i) __attribute__((always_inline)) { KV::rows(k[i], kt, row0, e, h, m32); },
                                   [&](int e, int i) __attribute__((always_inline)) { S = mma(k[i], q[e], S); });
         }
@@ -84,11 +84,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref));
         l += sum16(x);
-        Opnd<T> p[2];
+        Opnd<M> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
         {
-            Opnd<T> v[VA + 1];
+            Opnd<M> v[VA + 1];
             read_ahead<2 * MT, VA>(
                 [&](int e, int i) __attribute__((always_inline)) { KV::cols(v[i], vt, row0 + 16 * (e / MT), e % MT, lane); },
                 [&](int e, int i) __attribute__((always_inline)) { acc[e % MT] = mma(v[i], p[e / MT], acc[e % MT]); });
@@ -142,12 +142,13 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
 
 size_t window_forward_ws_bytes(const WindowDims& s) { return window_few(s) ? window_few_ws_bytes(s) : 0; }
 
-template <typename T, int D, int NW, int KT, int OCC, int KA, int VA>
+template <typename M, int D, int NW, int KT, int OCC, int KA, int VA>
 static hipError_t tiles_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first,
                           void* O, float* lse, hipStream_t st)
 {
-    auto* kernel = window_forward_kernel<T, D, NW, KT, OCC, KA, VA>;
-    constexpr size_t lds = 4 * Tile<T, D, KT>::BYTES;
+    using T = in_memory_t<M>;
+    auto* kernel = window_forward_kernel<M, D, NW, KT, OCC, KA, VA>;
+    constexpr size_t lds = 4 * Tile<M, D, KT>::BYTES;
     const hipError_t e = window_lds((const void*)kernel, lds);
     if (e != hipSuccess) return e;
     constexpr int QT = 32 * NW;
@@ -164,8 +165,8 @@ hipError_t launch_window_forward(const WindowDims& s, const void* Q, const void*
     if (s.dtype == MOBA_BF16)
         return s.D == 64 ? tiles_t<bf16_t, 64, 4, 64, 4, 0, 1>(s, Q, K, V, first, O, lse, st)
                          : tiles_t<bf16_t, 128, 4, 64, 2, 2, 3>(s, Q, K, V, first, O, lse, st);
-    return s.D == 64 ? tiles_t<float, 64, 4, 32, 3, 0, 0>(s, Q, K, V, first, O, lse, st)
-                     : tiles_t<float, 128, 4, 32, 2, 0, 0>(s, Q, K, V, first, O, lse, st);
+    return s.D == 64 ? tiles_t<Split, 64, 4, 32, 3, 0, 0>(s, Q, K, V, first, O, lse, st)
+                     : tiles_t<Split, 128, 4, 32, 1, 0, 0>(s, Q, K, V, first, O, lse, st);
 }
 
 }  // namespace moba

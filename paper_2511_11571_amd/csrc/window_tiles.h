@@ -17,6 +17,18 @@ namespace moba {
 template <typename T> struct Opnd;
 template <> struct Opnd<bf16_t> { Frag f; };
 template <> struct Opnd<float> { float v[8]; };
+// fp32 as three bf16 numbers, x = f0 + f1 + f2 exactly (24 bits; what is smaller than 2^-126 or rounds to infinity apart): six of
+// the nine products stand for one in fp32, for the others are below 2^-26 of it.  Six v_mfma_f32_32x32x16_bf16 take 192 cycles, the
+// eight fp32 products 512.  us, fp32 products -> these: 16 heads of 8192, W = 256, d = 64 forward 123 -> 71, backward 367 -> 221, d = 128
+// 215 -> 173, 823 -> 530; of 4096, dense, d = 128 1025 -> 444, 2190 -> 1300.  An infinity becomes a NaN in two of the parts, which
+// the second pass over sums that are not finite clears up.
+struct Split {};
+template <> struct Opnd<Split> { Frag f[3]; };
+
+// type in memory
+template <typename M> struct InMemory { using type = M; };
+template <> struct InMemory<Split> { using type = float; };
+template <typename M> using in_memory_t = typename InMemory<M>::type;
 
 __device__ __forceinline__ f32x16_t mma(const Opnd<bf16_t>& a, const Opnd<bf16_t>& b, f32x16_t c) { return mfma32(a.f, b.f, c); }
 __device__ __forceinline__ f32x16_t mma(const Opnd<float>& a, const Opnd<float>& b, f32x16_t c)
@@ -26,9 +38,39 @@ __device__ __forceinline__ f32x16_t mma(const Opnd<float>& a, const Opnd<float>&
     return c;
 }
 
+__device__ __forceinline__ f32x16_t mma(const Opnd<Split>& a, const Opnd<Split>& b, f32x16_t c)
+{
+    c = mfma32(a.f[2], b.f[0], c);
+    c = mfma32(a.f[0], b.f[2], c);
+    c = mfma32(a.f[1], b.f[1], c);
+    c = mfma32(a.f[1], b.f[0], c);
+    c = mfma32(a.f[0], b.f[1], c);
+    return mfma32(a.f[0], b.f[0], c);
+}
+__device__ __forceinline__ void split(Frag (&f)[3], const float* v)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a = v[2 * e], b = v[2 * e + 1];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const uint32_t x = pack2(a, b);
+            f[i].u[e] = x;
+            a -= __uint_as_float(x << 16);
+            b -= __uint_as_float(x & 0xffff0000u);
+        }
+    }
+}
+
 // eight neighbouring elements of a row in memory
 __device__ __forceinline__ void load_opnd(Opnd<bf16_t>& o, const bf16_t* p) { o.f.q = *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void load_opnd(Opnd<float>& o, const float* p) { Vec8<float>::load(p, o.v); }
+__device__ __forceinline__ void load_opnd(Opnd<Split>& o, const float* p)
+{
+    float v[8];
+    Vec8<float>::load(p, v);
+    split(o.f, v);
+}
 
 // eight elements of a result
 __device__ __forceinline__ void pack_opnd(Opnd<bf16_t>& o, const float* p)
@@ -41,6 +83,7 @@ __device__ __forceinline__ void pack_opnd(Opnd<float>& o, const float* p)
 #pragma unroll
     for (int e = 0; e < 8; ++e) o.v[e] = p[e];
 }
+__device__ __forceinline__ void pack_opnd(Opnd<Split>& o, const float* p) { split(o.f, p); }
 
 // a result's sixteen channels of column m to the 32 channels of row m that `to` points at.  bf16: the two lanes of a row swap
 // four channels each, so that both write eight neighbouring ones.
@@ -157,6 +200,61 @@ struct Tile {
                 const int r = 8 * (s >> 2) + 4 * h + (s & 3);
                 o.v[s] = *reinterpret_cast<const float*>(tile + (row0 + r) * RB + ((128 * mt) ^ (16 * ((m >> 2) ^ place(r)))) + 4 * (m & 3));
             }
+        }
+    }
+};
+
+// fp32 rows as three tiles of bf16, split on their way into LDS: once for all waves that read them
+template <int D, int ROWS>
+struct Tile<Split, D, ROWS> {
+    using Part = Tile<bf16_t, D, ROWS>;
+    static constexpr int PIECES = Part::PIECES, BYTES = 3 * Part::BYTES;
+    template <int NT>
+    static constexpr int pieces = 2 * ROWS * PIECES / NT;    // (eight fp32 elements make a piece of each part)
+    template <int NT>
+    static __device__ __forceinline__ void load(u32x4_t (&x)[2 * ROWS * PIECES / NT], const float* __restrict__ slice, int first, int last, int tid)
+    {
+        static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0, "whole pieces");
+#pragma unroll
+        for (int i = 0; i < ROWS * PIECES / NT; ++i) {
+            const int row = min(first + tid / PIECES + i * (NT / PIECES), last);
+            const u32x4_t* p = reinterpret_cast<const u32x4_t*>(slice + (int64_t)row * D + 8 * (tid % PIECES));
+            x[2 * i] = p[0];
+            x[2 * i + 1] = p[1];
+        }
+    }
+    template <int NT>
+    static __device__ __forceinline__ void store(const u32x4_t (&x)[2 * ROWS * PIECES / NT], unsigned char* tile, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < ROWS * PIECES / NT; ++i) {
+            const int row = tid / PIECES + i * (NT / PIECES);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[2 * i + e / 4][e % 4]);
+            Frag f[3];
+            split(f, v);
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                *reinterpret_cast<u32x4_t*>(tile + j * Part::BYTES + row * Part::RB + 16 * ((tid % PIECES) ^ Part::place(row))) = f[j].n;
+        }
+    }
+    static __device__ __forceinline__ void rows(Opnd<Split>& o, const unsigned char* tile, int row0, int c, int h, int m)
+    {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            Opnd<bf16_t> x;
+            Part::rows(x, tile + j * Part::BYTES, row0, c, h, m);
+            o.f[j] = x.f;
+        }
+    }
+    static __device__ __forceinline__ void cols(Opnd<Split>& o, const unsigned char* tile, int row0, int mt, int lane)
+    {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            Opnd<bf16_t> x;
+            Part::cols(x, tile + j * Part::BYTES, row0, mt, lane);
+            o.f[j] = x.f;
         }
     }
 };
