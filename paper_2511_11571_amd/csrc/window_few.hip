@@ -19,6 +19,10 @@ namespace moba {
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;            // keys a wave takes at a time
 
+// fp32 products by bf16 parts where four waves' tiles of them fit (98 KB at d = 64)
+template <typename T, int D>
+using FewOperand = std::conditional_t<sizeof(T) == 4 && D == 64, Split, T>;
+
 // parts of rows shared by workgroups: [slice][32 rows each][share][row][m (log2 units), l, O]
 template <int D>
 constexpr int kPartWords = D + 2;
@@ -65,7 +69,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
                                                                       float* __restrict__ part, int groups, int shares, int each)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
-    using KV = Tile<T, D, kFewKeys>;
+    using M = FewOperand<T, D>;
+    using KV = Tile<M, D, kFewKeys>;
     constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float wave_ref[NW][32], wave_l[NW][32];
@@ -79,7 +84,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     const T* Vs = V + (int64_t)skv * a.rows * D;
     const int idx = min(32 * group + m32, rows - 1);         // (rows past the end: the last one again, not stored)
     const int r = idx / a.G, s = skv * a.G + idx % a.G, t = t0 + r, lo = window_first(a, s, r);
-    Opnd<T> q[STEPS];
+    Opnd<M> q[STEPS];
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) load_opnd(q[e], Q + ((int64_t)s * a.q + r) * D + 16 * e + 8 * h);
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
@@ -100,7 +105,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
         f32x16_t S = f32x16_t{};
 #pragma unroll
         for (int e = 0; e < STEPS; ++e) {
-            Opnd<T> k;
+            Opnd<M> k;
             KV::rows(k, mine, 0, e, h, m32);
             S = mma(k, q[e], S);
         }
@@ -128,14 +133,14 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], c2, -ref));
         l += sum16(x);
-        Opnd<T> p[2];
+        Opnd<M> p[2];
         pack_opnd(p[0], x);
         pack_opnd(p[1], x + 8);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                Opnd<T> v;
+                Opnd<M> v;
                 KV::cols(v, mine + KV::BYTES, 16 * j, mt, lane);
                 acc[mt] = mma(v, p[j], acc[mt]);
             }
@@ -289,7 +294,8 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
                                        T* __restrict__ dQ, float* __restrict__ Dv, int skv, int group, unsigned char* smem)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
-    using KV = Tile<T, D, kFewKeys>;
+    using M = FewOperand<T, D>;
+    using KV = Tile<M, D, kFewKeys>;
     constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -299,7 +305,7 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     const int idx = min(32 * group + m32, rows - 1);
     const int r = idx / a.G, s = skv * a.G + idx % a.G, t = t0 + r, lo = window_first(a, s, r);
     const int64_t row = (int64_t)s * a.q + r;
-    Opnd<T> q[STEPS], g[STEPS];
+    Opnd<M> q[STEPS], g[STEPS];
     float Dr = 0.f;
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
@@ -341,7 +347,7 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
             for (int i = 0; i < 16; ++i) dP[i] = -Dr;
 #pragma unroll
             for (int e = 0; e < STEPS; ++e) {
-                Opnd<T> k, v;
+                Opnd<M> k, v;
                 KV::rows(k, mine, 0, e, h, m32);
                 S = mma(k, q[e], S);
                 KV::rows(v, mine + KV::BYTES, 0, e, h, m32);
@@ -358,14 +364,14 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = result_row(i) >= lo - u - 4 * h ? x[i] : 0.f;
             }
-            Opnd<T> p[2];
+            Opnd<M> p[2];
             pack_opnd(p[0], x);
             pack_opnd(p[1], x + 8);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    Opnd<T> k;
+                    Opnd<M> k;
                     KV::cols(k, mine, 16 * j, mt, lane);
                     acc[mt] = mma(k, p[j], acc[mt]);
                 }
@@ -440,7 +446,8 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
                                          unsigned char* smem)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
-    using QG = Tile<T, D, 32>;
+    using M = FewOperand<T, D>;
+    using QG = Tile<M, D, 32>;
     constexpr int WAVE_BYTES = 2 * QG::BYTES > 32 * D * 4 ? 2 * QG::BYTES : 32 * D * 4;
     __shared__ __align__(16) float stat_z[NW][32], stat_d[NW][32];
     __shared__ __align__(16) int stat_lo[NW][32];
@@ -448,7 +455,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int t0 = a.N - a.q, ku = 32 * tile, key = ku + m32;
-    Opnd<T> k[STEPS], v[STEPS];
+    Opnd<M> k[STEPS], v[STEPS];
     const int64_t own = ((int64_t)skv * a.rows + min(key, a.N - 1)) * D;
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
@@ -477,7 +484,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) ak[mt] = av[mt] = f32x16_t{};
     {
-        constexpr int P = QG::template pieces<kWave>, LANES = QG::PIECES;
+        constexpr int P = QG::template pieces<kWave>, LANES = QG::PIECES, LOADS = QG::LOADS;
         u32x4_t mq[P], mg[P], mo[OWN ? P : 1];
         float nz = 0.f, nd = 0.f;
         int nl = 0;
@@ -500,8 +507,11 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             if (h == 0) { sz[m32] = nz; sl[m32] = nl; }
             if constexpr (OWN) {
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    const float x = lanes_sum<LANES>(piece_dot(mo[j], mg[j], T()));
+                for (int j = 0; j < P / LOADS; ++j) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int e = 0; e < LOADS; ++e) x += piece_dot(mo[LOADS * j + e], mg[LOADS * j + e], T());
+                    x = lanes_sum<LANES>(x);
                     if (lane % LANES == 0) sd[lane / LANES + j * (kWave / LANES)] = -x;
                 }
             } else if (h == 0) {
@@ -517,7 +527,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             }
 #pragma unroll
             for (int e = 0; e < STEPS; ++e) {
-                Opnd<T> x;
+                Opnd<M> x;
                 QG::rows(x, mine, 0, e, h, m32);
                 S = mma(x, k[e], S);
                 QG::rows(x, mine + QG::BYTES, 0, e, h, m32);
@@ -562,12 +572,12 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                Opnd<T> pp, pd;
+                Opnd<M> pp, pd;
                 pack_opnd(pp, p + 8 * j);
                 pack_opnd(pd, ds + 8 * j);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    Opnd<T> x;
+                    Opnd<M> x;
                     QG::cols(x, mine + QG::BYTES, 16 * j, mt, lane);
                     av[mt] = mma(x, pp, av[mt]);
                     QG::cols(x, mine, 16 * j, mt, lane);
@@ -698,7 +708,7 @@ size_t window_few_ws_bytes(const WindowDims& s)
 template <typename T, int D>
 static size_t few_lds()
 {
-    return kFewWaves * std::max<size_t>(2 * Tile<T, D, kFewKeys>::BYTES, 32 * D * 4);
+    return kFewWaves * std::max<size_t>(2 * Tile<FewOperand<T, D>, D, kFewKeys>::BYTES, 32 * D * 4);
 }
 template <typename T, int D>
 static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first, void* O,

@@ -115,7 +115,7 @@ __device__ __forceinline__ float sum16(const float (&x)[16])
 // A tile of ROWS rows of D channels in LDS
 template <typename T, int D, int ROWS>
 struct Tile {
-    static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, BYTES = ROWS * RB;
+    static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, LOADS = 1, BYTES = ROWS * RB;      // a piece takes LOADS loads
     static __device__ __forceinline__ constexpr int place(int row)
     {
         return PIECES == 8 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3);
@@ -208,7 +208,7 @@ struct Tile {
 template <int D, int ROWS>
 struct Tile<Split, D, ROWS> {
     using Part = Tile<bf16_t, D, ROWS>;
-    static constexpr int PIECES = Part::PIECES, BYTES = 3 * Part::BYTES;
+    static constexpr int PIECES = Part::PIECES, LOADS = 2, BYTES = 3 * Part::BYTES;
     template <int NT>
     static constexpr int pieces = 2 * ROWS * PIECES / NT;    // (eight fp32 elements make a piece of each part)
     template <int NT>
