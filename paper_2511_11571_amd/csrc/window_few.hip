@@ -685,9 +685,16 @@ static int few_shares(const WindowDims& s)
 // bf16, d = 64: forward N = 1024, W = 256 11.1 | 7.1; 2048 11.6 | 13.0; 2048 dense 40.0 | 26.0; 8192 dense 235 | 241; 4 heads of
 // 8192, W = 2048 42.9 | 35.2; 4096 (16) 51.8 | 53.3.  Backward: N = 1024, W = 256 26.5 | 19.2; 2048 28.3 | 34.2; dense 4096
 // 236 | 194; 8192 567 | 668; d = 128, W = 256: N = 1024 46.1 | 42.5; 2048 50.1 | 80.1; dense 2048 176 | 162, 4096 412 | 502.
+// fp32, dense: d = 64 forward 4096 294 | 301, on 4 heads 240 | 303; 2048 106 | 86; 4 heads of 8192 400 | 293; d = 128 2048 189 | 206, 1024 98 | 61;
+// backward 2048 562 | 633, 1024 293 | 188.
 static bool few_tiles(const WindowDims& s, double tiles, double walk, double longest, double c)
 {
     return tiles * walk < c * longest - (s.D == 64 ? 24000 : 12000);
+}
+static double few_factor(const WindowDims& s, bool backward)
+{
+    if (s.dtype == MOBA_F32) return s.D == 64 ? 250 : 130;
+    return s.D == 64 ? 325 : backward ? 170 : 230;
 }
 static double all_pairs(const WindowDims& s)                 // of one head
 {
@@ -697,7 +704,7 @@ static double all_pairs(const WindowDims& s)                 // of one head
 bool window_few(const WindowDims& s)
 {
     const double tiles = (double)s.bh * s.q / 128;
-    return s.q <= 32 || tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : 230);
+    return s.q <= 32 || tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, few_factor(s, false));
 }
 size_t window_few_ws_bytes(const WindowDims& s)
 {
@@ -772,12 +779,12 @@ static hipError_t few_backward_t(const WindowDims& s, const void* Q, const void*
 bool window_few_dq(const WindowDims& s)
 {
     const double tiles = (double)s.bh * s.q / 128;
-    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, s.D == 64 ? 325 : s.dtype == MOBA_BF16 ? 170 : 230);
+    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.q, s.W, few_factor(s, true));
 }
 bool window_few_dkdv(const WindowDims& s)
 {
     const double tiles = (double)s.bhk * s.N / 128;
-    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.N, std::min(s.q, s.W), s.D == 64 ? 325 : s.dtype == MOBA_BF16 ? 170 : 230);
+    return tiles <= 128 || few_tiles(s, tiles, all_pairs(s) / s.N, std::min(s.q, s.W), few_factor(s, true));
 }
 
 hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
