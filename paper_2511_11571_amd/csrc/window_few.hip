@@ -22,6 +22,16 @@ constexpr int kFewKeys = 32;            // keys a wave takes at a time
 // fp32 products by bf16 parts where four waves' tiles of them fit (98 KB at d = 64)
 template <typename T, int D>
 using FewOperand = std::conditional_t<sizeof(T) == 4 && D == 64, Split, T>;
+// the forward at d = 128 has them as well: values follow the keys into the same place
+template <typename T>
+using FewForward = std::conditional_t<sizeof(T) == 4, Split, T>;
+template <typename T, int D>
+constexpr bool few_one = sizeof(T) == 4 && D == 128;
+template <typename M, int D, bool ONE>
+constexpr int few_wave_bytes()
+{
+    return std::max((ONE ? 1 : 2) * Tile<M, D, kFewKeys>::BYTES, 32 * D * 4);
+}
 
 // parts of rows shared by workgroups: [slice][32 rows each][share][row][m (log2 units), l, O]
 template <int D>
@@ -69,9 +79,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
                                                                       float* __restrict__ part, int groups, int shares, int each)
 {
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
-    using M = FewOperand<T, D>;
+    using M = FewForward<T>;
     using KV = Tile<M, D, kFewKeys>;
-    constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
+    constexpr bool ONE = few_one<T, D>;
+    constexpr int WAVE_BYTES = few_wave_bytes<M, D, ONE>();
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float wave_ref[NW][32], wave_l[NW][32];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
@@ -101,6 +112,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16_t{};
     float ref = kLowest, l = 0.f;
+    u32x4_t mk[KV::template pieces<kWave>], mv[KV::template pieces<kWave>];
     auto keys32 = [&](int u, bool late, bool early) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{};
 #pragma unroll
@@ -108,6 +120,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             Opnd<M> k;
             KV::rows(k, mine, 0, e, h, m32);
             S = mma(k, q[e], S);
+        }
+        if constexpr (ONE) {
+            KV::template store<kWave>(mv, mine, lane);
+            if (u + NW * kFewKeys < end) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
         }
         float x[16], top = -INFINITY;
 #pragma unroll
@@ -141,12 +157,11 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 Opnd<M> v;
-                KV::cols(v, mine + KV::BYTES, 16 * j, mt, lane);
+                KV::cols(v, mine + (ONE ? 0 : KV::BYTES), 16 * j, mt, lane);
                 acc[mt] = mma(v, p[j], acc[mt]);
             }
     };
     {
-        u32x4_t mk[KV::template pieces<kWave>], mv[KV::template pieces<kWave>];
         int u = first + wave * kFewKeys;
         if (u < end) {
             KV::template load<kWave>(mk, Ks, u, a.N - 1, lane);
@@ -155,10 +170,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
         for (; u < end; u += NW * kFewKeys) {
             // (the wave's own LDS: its reads of the keys before are done before these stores, in order)
             KV::template store<kWave>(mk, mine, lane);
-            KV::template store<kWave>(mv, mine + KV::BYTES, lane);
+            if constexpr (!ONE) KV::template store<kWave>(mv, mine + KV::BYTES, lane);
             if (u + NW * kFewKeys < end) {
                 KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
-                KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
+                if constexpr (!ONE) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
             }
             keys32(u, u + kFewKeys - 1 > t_min, u < lo_max);
         }
@@ -296,7 +311,7 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
     using M = FewOperand<T, D>;
     using KV = Tile<M, D, kFewKeys>;
-    constexpr int WAVE_BYTES = 2 * KV::BYTES > 32 * D * 4 ? 2 * KV::BYTES : 32 * D * 4;
+    constexpr int WAVE_BYTES = few_wave_bytes<M, D, false>();
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int rows = a.G * a.q, t0 = a.N - a.q;
@@ -448,7 +463,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
     constexpr int NW = kFewWaves, STEPS = D / 16, MT = D / 32;
     using M = FewOperand<T, D>;
     using QG = Tile<M, D, 32>;
-    constexpr int WAVE_BYTES = 2 * QG::BYTES > 32 * D * 4 ? 2 * QG::BYTES : 32 * D * 4;
+    constexpr int WAVE_BYTES = few_wave_bytes<M, D, false>();
     __shared__ __align__(16) float stat_z[NW][32], stat_d[NW][32];
     __shared__ __align__(16) int stat_lo[NW][32];
     __shared__ int range[NW];
@@ -713,10 +728,7 @@ size_t window_few_ws_bytes(const WindowDims& s)
 }
 
 template <typename T, int D>
-static size_t few_lds()
-{
-    return kFewWaves * std::max<size_t>(2 * Tile<FewOperand<T, D>, D, kFewKeys>::BYTES, 32 * D * 4);
-}
+constexpr size_t few_lds = kFewWaves * few_wave_bytes<FewOperand<T, D>, D, false>();
 template <typename T, int D>
 static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const void* V, const int32_t* first, void* O,
                         float* lse, void* ws, hipStream_t st)
@@ -725,7 +737,7 @@ static hipError_t few_t(const WindowDims& s, const void* Q, const void* K, const
     const int groups = few_groups(s), shares = few_shares(s);
     // keys of a share: whole turns of 32 (the first keys of a group start at a multiple of 32 up to 31 before its own)
     const int each = ((few_keys(s) + 31 + shares - 1) / shares + kFewKeys - 1) / kFewKeys * kFewKeys;
-    const size_t lds = few_lds<T, D>();
+    constexpr size_t lds = kFewWaves * few_wave_bytes<FewForward<T>, D, few_one<T, D>>();
     auto* kernel = window_few_kernel<T, D>;
     const hipError_t g = window_lds((const void*)kernel, lds);
     if (g != hipSuccess) return g;
@@ -742,10 +754,10 @@ template <typename T, int D>
 static hipError_t few_dq_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse, const void* dO,
                            const int32_t* first, void* dQ, float* Dv, hipStream_t st)
 {
-    const hipError_t e = window_lds((const void*)window_few_dq_kernel<T, D>, few_lds<T, D>());
+    const hipError_t e = window_lds((const void*)window_few_dq_kernel<T, D>, few_lds<T, D>);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((window_few_dq_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, few_groups(s))), dim3(kFewWaves * kWave),
-                       (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO,
+                       (few_lds<T, D>), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, (const T*)O, lse, (const T*)dO,
                        (T*)dQ, Dv, few_groups(s));
     return hipGetLastError();
 }
@@ -753,11 +765,11 @@ template <typename T, int D>
 static hipError_t few_dkdv_t(const WindowDims& s, const void* Q, const void* K, const void* V, const float* lse, const void* dO,
                              const int32_t* first, void* dK, void* dV, float* Dv, hipStream_t st)
 {
-    const hipError_t e = window_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>());
+    const hipError_t e = window_lds((const void*)window_few_dkdv_kernel<T, D>, few_lds<T, D>);
     if (e != hipSuccess) return e;
     const int ktiles = (s.N + 31) / 32;
     hipLaunchKernelGGL((window_few_dkdv_kernel<T, D>), dim3((unsigned)schedule_grid(s.bhk, ktiles)), dim3(kFewWaves * kWave),
-                       (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV,
+                       (few_lds<T, D>), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V, lse, (const T*)dO, (T*)dK, (T*)dV,
                        Dv, ktiles);
     return hipGetLastError();
 }
@@ -766,12 +778,12 @@ template <typename T, int D>
 static hipError_t few_backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
                                  const void* dO, const int32_t* first, void* dQ, void* dK, void* dV, float* Dv, hipStream_t st)
 {
-    const hipError_t e = window_lds((const void*)window_few_backward_kernel<T, D>, few_lds<T, D>());
+    const hipError_t e = window_lds((const void*)window_few_backward_kernel<T, D>, few_lds<T, D>);
     if (e != hipSuccess) return e;
     const int groups = few_groups(s), ktiles = (s.N + 31) / 32;
     const int grid_q = schedule_grid(s.bhk, groups), first_k = (grid_q + kXcds - 1) / kXcds * kXcds;
     hipLaunchKernelGGL((window_few_backward_kernel<T, D>), dim3((unsigned)(first_k + schedule_grid(s.bhk, ktiles))),
-                       dim3(kFewWaves * kWave), (few_lds<T, D>()), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V,
+                       dim3(kFewWaves * kWave), (few_lds<T, D>), st, window_args(s, first), (const T*)Q, (const T*)K, (const T*)V,
                        (const T*)O, lse, (const T*)dO, (T*)dQ, (T*)dK, (T*)dV, Dv, groups, grid_q, first_k, ktiles);
     return hipGetLastError();
 }
