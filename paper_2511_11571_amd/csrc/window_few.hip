@@ -9,7 +9,7 @@
 //
 // What bounds it: with many keys, how fast they come in -- 4 positions of 16 heads on 4 against 131109 keys, d = 128 50 us, 5.4 TB/s (a copy of
 // that size runs at 5.4), 6 of them the second kernel; with few, the chain of steps: a position against 256 keys 4.4 us, fp32, 2
-// heads of 2048, W = 256 12 us forward and 25 backward (a lot of 32 x 32 is 4 us of fp32 products for dK and dV).
+// heads of 2048, W = 256 12 us forward and 22 backward.
 #include <algorithm>
 
 #include "window_tiles.h"
@@ -700,7 +700,7 @@ static int few_shares(const WindowDims& s)
 // bf16, d = 64: forward N = 1024, W = 256 11.1 | 7.1; 2048 11.6 | 13.0; 2048 dense 40.0 | 26.0; 8192 dense 235 | 241; 4 heads of
 // 8192, W = 2048 42.9 | 35.2; 4096 (16) 51.8 | 53.3.  Backward: N = 1024, W = 256 26.5 | 19.2; 2048 28.3 | 34.2; dense 4096
 // 236 | 194; 8192 567 | 668; d = 128, W = 256: N = 1024 46.1 | 42.5; 2048 50.1 | 80.1; dense 2048 176 | 162, 4096 412 | 502.
-// fp32, dense: d = 64 forward 4096 294 | 301, on 4 heads 240 | 303; 2048 106 | 86; 4 heads of 8192 400 | 293; d = 128 2048 189 | 206, 1024 98 | 61;
+// fp32, dense: d = 64 forward 4096 294 | 301, on 4 heads 240 | 303; 2048 106 | 86; 4 heads of 8192 400 | 293; d = 128 2048 189 | 170, 4096 421 | 604;
 // backward 2048 562 | 633, 1024 293 | 188.
 static bool few_tiles(const WindowDims& s, double tiles, double walk, double longest, double c)
 {
@@ -708,7 +708,7 @@ static bool few_tiles(const WindowDims& s, double tiles, double walk, double lon
 }
 static double few_factor(const WindowDims& s, bool backward)
 {
-    if (s.dtype == MOBA_F32) return s.D == 64 ? 250 : 130;
+    if (s.dtype == MOBA_F32) return s.D == 64 ? 250 : backward ? 130 : 180;
     return s.D == 64 ? 325 : backward ? 170 : 230;
 }
 static double all_pairs(const WindowDims& s)                 // of one head
