@@ -341,7 +341,8 @@ typedef struct moba_window_shape {
  * where two start at the same address).
  * Tensors of dtype and ws start on 16-byte boundaries, lse and first_key on 4-byte ones (else MOBA_EINVAL).  kv_len <= kv_rows <= 2^24,
  * q_len <= kv_len, batch * heads <= 65535; otherwise MOBA_EINVAL or, for the two limits,
- * MOBA_EUNSUPPORTED.  Results are the same in every run.
+ * MOBA_EUNSUPPORTED.  Results are the same in every run.  fp32: products are made of
+ * three parts of 8 bits each; numbers below 2^-108 count with fewer than 24.
  */
 int moba_window_workspace(const moba_window_shape* shape, size_t* fwd_ws, size_t* bwd_ws);
 int moba_window_forward(const moba_window_shape* shape, const void* Q, const void* K, const void* V,

@@ -17,11 +17,11 @@ namespace moba {
 template <typename T> struct Opnd;
 template <> struct Opnd<bf16_t> { Frag f; };
 template <> struct Opnd<float> { float v[8]; };
-// fp32 as three bf16 numbers, x = f0 + f1 + f2 exactly (24 bits; what is smaller than 2^-126 or rounds to infinity apart): six of
+// fp32 as three bf16 numbers, x = f0 + f1 + f2 exactly (24 bits; below 2^-108 the last of them may be lost): six of
 // the nine products stand for one in fp32, for the others are below 2^-26 of it.  Six v_mfma_f32_32x32x16_bf16 take 192 cycles, the
 // eight fp32 products 512.  us, fp32 products -> these: 16 heads of 8192, W = 256, d = 64 forward 123 -> 71, backward 367 -> 221, d = 128
-// 215 -> 173, 823 -> 530; of 4096, dense, d = 128 1025 -> 444, 2190 -> 1300.  An infinity becomes a NaN in two of the parts, which
-// the second pass over sums that are not finite clears up.
+// 215 -> 173, 823 -> 530; of 4096, dense, d = 128 1025 -> 444, 2190 -> 1300.  An infinity (or what rounds to one) becomes a NaN
+// in two of the parts, which the second pass over sums that are not finite clears up.
 struct Split {};
 template <> struct Opnd<Split> { Frag f[3]; };
 
