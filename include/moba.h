@@ -350,7 +350,9 @@ int moba_window_forward(const moba_window_shape* shape, const void* Q, const voi
 
 /*
  * Its backward, which recomputes the probabilities: D = rowsum(dO o O), P = exp(scale * Q K^T - lse),
- * dV = P^T dO, dS = P o (dO V^T - D), dQ = scale * dS K, dK = scale * dS^T Q.
+ * dV = P^T dO, dS = P o (dO V^T - D), dQ = scale * dS K, dK = scale * dS^T Q.  A row that attends one key
+ * has no gradient with respect to its logit: its dQ is zero and it adds nothing to dK, not a rounding
+ * (infinities and NaN among its own values give NaN).
  *   Q, O, dO   in   [b,heads,q_len,d] dtype;   lse in [b,heads,q_len] fp32 (from moba_window_forward)
  *   dQ         out  [b,heads,q_len,d] dtype
  *   dK, dV     out  [b,kv,kv_rows,d] dtype, rows below kv_len, summed over the query heads that share the

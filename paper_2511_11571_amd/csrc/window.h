@@ -111,10 +111,10 @@ __device__ __forceinline__ void plain_forward_row(const WindowArgs& a, const T* 
     if (lane == 0) lse[row] = empty ? -INFINITY : (m + fast_log2(l)) * kLn2;
 }
 
-// Factor of the sums of dQ and of dK.  The gradient with respect to the one logit of a row that attends one key is zero,
-// and dO . v - D only as far as sums in different orders agree.
-__device__ __forceinline__ float dq_factor(const WindowArgs& a, int lo, int t) { return lo < t ? a.scale : 0.f; }
-__device__ __forceinline__ float dk_factor(const WindowArgs& a) { return a.W > 1 ? a.scale : 0.f; }
+// The gradient with respect to the one logit of a row that attends one key is zero, and dO . v - D only as far as sums in
+// different orders agree.  So dS of such a row is multiplied by zero, which leaves a NaN one; for dQ its sum is.
+__device__ __forceinline__ float ds_factor(int lo, int t) { return lo < t ? 1.f : 0.f; }
+__device__ __forceinline__ float dq_factor(const WindowArgs& a, int lo, int t) { return a.scale * ds_factor(lo, t); }
 
 template <typename T, int D>
 __device__ __forceinline__ void plain_dq_row(const WindowArgs& a, const T* __restrict__ Q, const T* __restrict__ K,
@@ -158,12 +158,13 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
         const int64_t base = (int64_t)s * a.q;
         for (int r0 = r_lo; r0 < r_hi && !(all_nan(ak) && all_nan(av)); r0 += kWave) {
             const int r = r0 + lane;
-            const bool on = r < r_hi && window_first(a, s, r) <= u;
+            const int lo = r < r_hi ? window_first(a, s, r) : 0;
+            const bool on = r < r_hi && lo <= u;
             float p = 0.f, ds = 0.f;
             if (on) {
                 p = fast_exp2(fmaf(row_dot<T, D>(Q + (base + r) * D, K + key), a.scale * kLog2e, -lse[base + r] * kLog2e));
                 const float Dr = OWN ? row_dot<T, D>(dO + (base + r) * D, O + (base + r) * D) : Dv[base + r];
-                ds = p * (row_dot<T, D>(dO + (base + r) * D, V + key) - Dr);
+                ds = p * (row_dot<T, D>(dO + (base + r) * D, V + key) - Dr) * ds_factor(lo, a.N - a.q + r);
             }
             for (uint64_t left = __ballot(on); left; left &= left - 1) {
                 const int j = __builtin_ctzll(left);
@@ -179,7 +180,7 @@ __device__ __forceinline__ void plain_dkdv_key(const WindowArgs& a, const T* __r
     }
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-        dK[key + lane + 64 * c] = from_f32<T>(ak[c] * dk_factor(a));
+        dK[key + lane + 64 * c] = from_f32<T>(ak[c] * a.scale);
         dV[key + lane + 64 * c] = from_f32<T>(av[c]);
     }
 }

@@ -221,9 +221,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) ak[mt] = av[mt] = f32x16_t{};
 
-    // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys
+    // rows r .. r + 31 of the tile in LDS (from its row row0 on) against the wave's keys; late: some key is a row's own or lies
+    // behind it; alone: some row may attend its own key and no other
     auto rows32 = [&](const unsigned char* qt, const unsigned char* gt, const float* sz, const float* sd, const int* sl, int row0, int r,
-                      bool late, bool early) __attribute__((always_inline)) {
+                      bool late, bool early, bool alone) __attribute__((always_inline)) {
         f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
@@ -262,6 +263,11 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             const int least = key - t0 - r - 4 * h;
 #pragma unroll
             for (int i = 0; i < 16; ++i) only(i, result_row(i) >= least);
+            if (alone) {
+                const uint32_t rows = (uint32_t)__ballot(ds_factor(sl[row0 + m32], t0 + r + m32) == 0.f) >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] *= rows >> result_row(i) & 1 ? 0.f : 1.f;
+            }
         }
         if (early) {
             // ... up to the last that exists and whose window still holds it; with first keys, by each row's own
@@ -346,12 +352,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             for (int x = 0; x < QT / 32; ++x) {
                 const int r = r_here + 32 * x;
                 if (r >= a.q || t0 + min(r + 31, a.q - 1) < ku || ku >= a.N || lo_here[x].x > ku + 31) continue;
-                rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, t0 + r < ku + 31, r + 31 >= a.q || lo_here[x].y > ku);
+                rows32(qt, qt + QG::BYTES, stat_z[buf], stat_d[buf], stat_lo[buf], 32 * x, r, t0 + r <= ku + 31, r + 31 >= a.q || lo_here[x].y > ku,
+                       lo_here[x].y >= t0 + r);
             }
             if (more) arrived(buf ^ 1);
         }
     }
-    const float k_factor = dk_factor(a);
     float most = 0.f;
     if (key < a.N) {
         const int64_t at = ((int64_t)skv * a.rows + key) * D;
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
             float x[16], y[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[i] = ak[mt][i] * k_factor;
+                x[i] = ak[mt][i] * a.scale;
                 y[i] = av[mt][i];
                 most = max_nan(max_nan(most, fabsf(x[i])), fabsf(y[i]));
             }

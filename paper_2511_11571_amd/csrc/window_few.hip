@@ -532,7 +532,9 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             } else if (h == 0) {
                 sd[m32] = nd;
             }
-            const bool late = t0 + r <= ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;   // late: a row's own key is among them
+            // late: some key is a row's own or lies behind it; alone: the rows that attend their own key and no other
+            const bool late = t0 + r <= ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;
+            const uint32_t alone = (uint32_t)__ballot(ds_factor(nl, t0 + r + m32) == 0.f);
             if (i + NW < total) fetch(i + NW);
             f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
@@ -567,11 +569,10 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
                 const int least = key - t0 - r - 4 * h;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) only(j, result_row(j) >= least);
-                // rows that attend their own key alone (sequences of one in a packed batch)
+                if (alone) {
+                    const uint32_t rows = alone >> (4 * h);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int o = result_row(j) + 4 * h;
-                    ds[j] = sl[o] < t0 + r + o ? ds[j] : 0.f;
+                    for (int j = 0; j < 16; ++j) ds[j] *= rows >> result_row(j) & 1 ? 0.f : 1.f;
                 }
             }
             if (early) {
@@ -624,7 +625,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             Vec8<T>::store(to + ((int64_t)skv * a.rows + ku + c) * D + ch0 + e, x);
         }
     };
-    out(ak, dK, dk_factor(a));
+    out(ak, dK, a.scale);
     __syncthreads();
     out(av, dV, 1.f);
     // keys that are not finite once more, from their own pairs alone
