@@ -365,7 +365,8 @@ int moba_window_backward(const moba_window_shape* shape, const void* Q, const vo
 /*
  * first_key of a packed batch: offsets[i] of the sequence that row t belongs to, for every row below
  * offsets[num_seqs] (device arrays; seq_offsets for the packed layout, pad_offsets for the padded one,
- * whose padding rows then attend like rows of the sequence before them).
+ * whose padding rows then attend like rows of the sequence before them).  Both arrays start on 4-byte boundaries
+ * and do not overlap (MOBA_EINVAL where they do not, or start at the same address).
  */
 int moba_varlen_first_key(int32_t num_seqs, const int32_t* offsets, int32_t tokens, int32_t* first_key, void* stream);
 

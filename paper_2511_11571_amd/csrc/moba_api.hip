@@ -653,6 +653,7 @@ int moba_window_backward(const moba_window_shape* shape, const void* Q, const vo
 int moba_varlen_first_key(int32_t num_seqs, const int32_t* offsets, int32_t tokens, int32_t* first_key, void* stream)
 {
     if (num_seqs <= 0 || tokens < 0 || !offsets || (tokens > 0 && !first_key)) return MOBA_EINVAL;
+    if (!aligned(4, {offsets, first_key}) || first_key == offsets) return MOBA_EINVAL;
     return hip_status(launch_varlen_first_key(offsets, num_seqs, tokens, first_key, (hipStream_t)stream));
 }
 

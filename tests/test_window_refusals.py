@@ -170,3 +170,15 @@ def test_the_structures_are_laid_out_as_the_header_says(tmp_path):
         want.append(str(ctypes.sizeof(c)))
         want += ["%d %d %d" % (getattr(c, n).offset, getattr(c, n).size, kinds[t]) for n, t in c._fields_]
     assert subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")[:-1] == want
+
+
+@no_device
+def test_first_key_pointers(lib):
+    f = lib.moba_varlen_first_key
+    good = (2, ctypes.c_void_p(_at(0)), 5, ctypes.c_void_p(_at(1)), None)
+    assert f(*good) not in (0, EINVAL)
+    for i, bad in ((0, 0), (0, -1), (1, None), (1, ctypes.c_void_p(_at(0) + 2)), (2, -1), (3, None), (3, ctypes.c_void_p(_at(1) + 1)),
+                   (3, ctypes.c_void_p(_at(0)))):
+        args = list(good)
+        args[i] = bad
+        assert f(*args) == EINVAL, (i, bad)
