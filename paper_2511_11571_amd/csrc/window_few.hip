@@ -44,6 +44,7 @@ struct WaveSums {
     static constexpr int NW = kFewWaves, TPR = NW * kWave / 32, CH = D / TPR;
     static __device__ __forceinline__ void put(unsigned char* mine, const f32x16_t (&acc)[D / 32], int h, int m32)
     {
+        wave_lds_order();
 #pragma unroll
         for (int mt = 0; mt < D / 32; ++mt)
 #pragma unroll
@@ -122,7 +123,9 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             S = mma(k, q[e], S);
         }
         if constexpr (ONE) {
+            wave_lds_order();
             KV::template store<kWave>(mv, mine, lane);
+            wave_lds_order();
             if (u + NW * kFewKeys < end) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
         }
         float x[16], top = -INFINITY;
@@ -168,9 +171,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
         }
         for (; u < end; u += NW * kFewKeys) {
-            // (the wave's own LDS: its reads of the keys before are done before these stores, in order)
+            wave_lds_order();                                // (the wave's own LDS: no other wave has to be waited for)
             KV::template store<kWave>(mk, mine, lane);
             if constexpr (!ONE) KV::template store<kWave>(mv, mine + KV::BYTES, lane);
+            wave_lds_order();
             if (u + NW * kFewKeys < end) {
                 KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
                 if constexpr (!ONE) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
@@ -351,8 +355,10 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
             KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
         }
         for (; u <= t_max; u += NW * kFewKeys) {
+            wave_lds_order();
             KV::template store<kWave>(mk, mine, lane);
             KV::template store<kWave>(mv, mine + KV::BYTES, lane);
+            wave_lds_order();
             if (u + NW * kFewKeys <= t_max) {
                 KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
                 KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
@@ -517,6 +523,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
         if (wave < total) fetch(wave);
         for (int i = wave; i < total; i += NW) {
             const int r = begin + i % per * 32;
+            wave_lds_order();
             QG::template store<kWave>(mq, mine, lane);
             QG::template store<kWave>(mg, mine + QG::BYTES, lane);
             if (h == 0) { sz[m32] = nz; sl[m32] = nl; }
@@ -532,6 +539,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
             } else if (h == 0) {
                 sd[m32] = nd;
             }
+            wave_lds_order();
             // late: some key is a row's own or lies behind it; alone: the rows that attend their own key and no other
             const bool late = t0 + r <= ku + 31, early = r + 31 >= a.q || __ballot(nl > ku) != 0;
             const uint32_t alone = (uint32_t)__ballot(ds_factor(nl, t0 + r + m32) == 0.f);

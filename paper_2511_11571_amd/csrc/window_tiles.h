@@ -259,6 +259,14 @@ struct Tile<Split, D, ROWS> {
     }
 };
 
+// Between a wave's accesses to LDS of which one lane's writes meet another lane's reads, or the other way round.  The hardware
+// keeps a wave's LDS accesses in order; this says so to the compiler, and costs no instruction.
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Two tiles, one behind the other in LDS, on their way while a workgroup of NT threads works on two others: through
