@@ -164,8 +164,8 @@ struct Tile {
             const int row = tid / PIECES + i * (NT / PIECES);
             const char* at = reinterpret_cast<const char*>(slice) + (int64_t)min(first + row, last) * RB + 16 * ((tid % PIECES) ^ place(row));
             const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
-            // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS.  It keeps nothing in m0.)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory");
+            // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory", "m0");
         }
     }
 
