@@ -379,7 +379,8 @@ int moba_varlen_first_key(int32_t num_seqs, const int32_t* offsets, int32_t toke
  * that a pair keeps in a context stretched beyond orig_len positions, by its turns within those,
  *   keep_i = clamp((orig_len g_i / (2 pi) - band_low) / (band_high - band_low), 0, 1).
  * Pair i is channels (i, i + rot_dim / 2), or with `interleaved` (2 i, 2 i + 1).  Channels from rot_dim
- * on are copied.  Angles are taken in 64 bits, products in fp32.
+ * on are copied.  Angles are taken in 64 bits, products in fp32.  Frequencies that times 2^32 are no finite
+ * number are refused (MOBA_EINVAL).
  */
 typedef struct moba_rope_shape {
     int32_t batch, heads;  /* heads of Q                                                         */

@@ -291,6 +291,7 @@ int rope_args(const moba_rope_shape* sh, RopeArgs& a)
             f *= keep + (1.0 - keep) / sh->scale_factor;
         }
         a.freq[i] = f / two_pi;
+        if (!(a.freq[i] * 4294967296.0 <= 1.7976931348623157e308)) return MOBA_EINVAL;     // (positions: up to 2^31 + 2^24)
     }
     return MOBA_OK;
 }

@@ -182,3 +182,16 @@ def test_first_key_pointers(lib):
         args = list(good)
         args[i] = bad
         assert f(*args) == EINVAL, (i, bad)
+
+
+@no_device
+def test_rotary_frequencies_beyond_64_bits(lib):
+    """An angle that is not finite has no cosine: position times frequency has to be a number, at any position."""
+    for kw in (dict(theta=5e-324), dict(theta=1e-308, head_dim=128), dict(scale_factor=1e-307), dict(scale_factor=5e-324),
+               dict(theta=1e-200, scale_factor=1e-150), dict(scale_factor=1e-307, orig_len=8192, band_low=1e5, band_high=1e6)):
+        for f in _rope_calls(lib):
+            assert _call(f, _rope(**kw), ROPE) == EINVAL, kw
+    for kw in (dict(theta=1e-200), dict(theta=1e300), dict(scale_factor=1e-200), dict(scale_factor=1e300), dict(theta=5e-324, rot_dim=2),
+               dict(scale_factor=1.0, orig_len=1e300)):
+        for f in _rope_calls(lib):
+            assert _call(f, _rope(**kw), ROPE) not in (0, EINVAL), kw
