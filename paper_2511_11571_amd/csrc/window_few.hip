@@ -820,12 +820,16 @@ hipError_t launch_window_few_dq(const WindowDims& s, const void* Q, const void* 
 
 // One launch for both directions' kernels gains where together they do not fill the chip and loses elsewhere, for dK and dV read O
 // for every 32 keys again.  us, two launches | one, bf16: 16 heads of 100, d = 64 9.9 | 6.2; 16 of 512, W = 256 13.6 | 12.0, d = 128
-// 22.1 | 26.2; 1 of 4096 22.5 | 19.3, of 8192 27.0 | 30.4; 16 on 4 of 512 33.5 | 44.8.  fp32, d = 64: 4 of 1024,
-// W = 256 32.6 | 21.3, 4 of 2048 34.7 | 36.1, dense 115 | 91, 4096 249 | 268; d = 128: 4 of 1024 70.8 | 59.6, of 2048 75.3 | 92.9.
+// 22.1 | 26.2; 1 of 4096 22.5 | 19.3, of 8192 27.0 | 30.4; 16 on 4 of 512 33.5 | 44.8.  fp32, d = 128: 4 of 1024 70.8 | 59.6,
+// of 2048 75.3 | 92.9; d = 64, W = 256: 5 of 1000 (320 workgroups) 31.9 | 29.4, 6 of 1000 31.6 | 31.5; 512 workgroups gain where the
+// window is half of the keys or more, for the longest walks of either kernel then begin early: dense 16 of 512 37.1 | 35.2, 8 of 1024 61.0 | 46.7, 4 of
+// 2048 109 | 82, 1 of 8192 400 | 295; 8 of 1024, W = 512 43.3 | 41.8, W = 256 31.2 | 31.2; 4 of 2048, W = 1024 68.0 | 68.8, W = 512
+// 43.9 | 44.8; 2 of 4096, W = 1024 69.0 | 72.2, W = 256 32.1 | 33.5.  Dense 4 of 4096 (1024 workgroups) 249 | 268.
 bool window_few_both(const WindowDims& s)
 {
     const int64_t groups = (int64_t)s.bhk * (few_groups(s) + (s.N + 31) / 32);
-    return window_few_dq(s) && window_few_dkdv(s) && groups <= (s.D == 64 && s.G == 1 ? 512 : 256);
+    const int most = s.D != 64 || s.G != 1 ? 256 : s.dtype == MOBA_BF16 || s.W >= s.N / 2 ? 512 : 384;
+    return window_few_dq(s) && window_few_dkdv(s) && groups <= most;
 }
 
 hipError_t launch_window_few_backward(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O, const float* lse,
