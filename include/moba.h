@@ -329,7 +329,9 @@ typedef struct moba_window_shape {
  *   O = sum_u p_u v_u, p = softmax(scale * q . k_u), lse = log sum_u exp(scale * q . k_u).
  * A row whose first_key lies behind t attends nothing: O = 0, lse = -inf, zero gradients, whatever its
  * Q and dO hold.  A row's results do not depend on what stands in keys, values and queries outside its
- * pairs, infinities and NaN included (calls that meet those take longer).
+ * pairs, infinities and NaN included.  Padding at either end -- keys that first_key leaves to no row, rows that attend
+ * nothing -- may hold anything and changes no bit.  Infinities and NaN elsewhere, in a neighbouring sequence say, cost time: rows
+ * of the same tile are summed once more, each from its own pairs, in an order that may give other last bits.
  *   Q          in   [b,heads,q_len,d] dtype
  *   K, V       in   [b,kv,kv_rows,d] dtype
  *   first_key  in   [b,q_len] int32, or NULL = 0: first key of the sequence that the row belongs to, for

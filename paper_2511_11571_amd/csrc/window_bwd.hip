@@ -24,25 +24,29 @@
 
 namespace moba {
 
-// what the kernel for dK and dV finds: D of every row and, with first keys, the smallest and largest of 32 rows each
+// what the kernel for dK and dV finds: D of every row and, with first keys, for 32 rows each (x, y) the smallest and largest of
+// them and (z, w) the first and last row that attends something.  Rows that attend nothing count as INT_MAX in x.
 struct WindowLeft {
     const float* D;             // [bh][q]
-    const int2* lo;             // [batch][ceil(q / 32)]; rows that attend nothing count as INT_MAX in the smallest
+    const int4* lo;             // [batch][ceil(q / 32)]
 };
 
 // those, where the kernel for dQ by tiles has not left them: a wave per two lots of 32 rows
-__global__ __launch_bounds__(256) void window_lo_kernel(WindowArgs a, int2* __restrict__ lo, int lots)
+__global__ __launch_bounds__(256) void window_lo_kernel(WindowArgs a, int4* __restrict__ lo, int lots)
 {
     const int i = blockIdx.x * 8 + threadIdx.x / 32, b = blockIdx.y;
     const int r = min(i * 32 + (int)threadIdx.x % 32, a.q - 1);
     const int first = window_first(a, b * a.heads, r);
-    int least = first <= a.N - a.q + r ? first : 0x7fffffff, most = first;
+    const bool live = first <= a.N - a.q + r;
+    int least = live ? first : 0x7fffffff, most = first, live_min = live ? r : 0x7fffffff, live_max = live ? r : -1;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         least = min(least, __shfl_xor(least, o, 32));
         most = max(most, __shfl_xor(most, o, 32));
+        live_min = min(live_min, __shfl_xor(live_min, o, 32));
+        live_max = max(live_max, __shfl_xor(live_max, o, 32));
     }
-    if (i < lots && threadIdx.x % 32 == 0) lo[(int64_t)b * lots + i] = make_int2(least, most);
+    if (i < lots && threadIdx.x % 32 == 0) lo[(int64_t)b * lots + i] = make_int4(least, most, live_min, live_max);
 }
 
 template <typename M, int D, int NW, int KT, int OCC, int QA, int QB, typename T = in_memory_t<M>>
@@ -50,12 +54,12 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
                                                               const T* __restrict__ V, const T* __restrict__ O,
                                                               const float* __restrict__ lse, const T* __restrict__ dO,
                                                               T* __restrict__ dQ, float* __restrict__ Dv,
-                                                              int2* __restrict__ lo_out, int ntiles)
+                                                              int4* __restrict__ lo_out, int ntiles)
 {
     constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
     using KV = Tile<M, D, KT>;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int wg_lo[NW];
+    __shared__ int2 wg_keys[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int skv, pos;
@@ -83,10 +87,10 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     const bool mine = r0 + m32 < a.q;
     if (mine && h == 0) Dv[row] = Dr;
     const float z = lse[row] * kLog2e, c2 = a.scale * kLog2e;
-    const WaveKeys w = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_lo);
+    const WaveKeys w = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_keys);
     if (lo_out && lane == 0 && s % a.heads == 0 && r0 < a.q)
-        lo_out[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int2(w.lo_min, w.lo_max);
-    const int begin = w.begin, end = t0 + min((tile + 1) * QT, a.q);
+        lo_out[(int64_t)(s / a.heads) * ((a.q + 31) / 32) + r0 / 32] = make_int4(w.lo_min, w.lo_max, w.live_min - t0, w.live_max - t0);
+    const int begin = w.begin, end = min(t0 + min((tile + 1) * QT, a.q), w.high + 1);
 
     f32x16_t acc[MT];
 #pragma unroll
@@ -130,14 +134,14 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dq_kernel(WindowArgs a,
     };
     if (begin < end) {
         Coming<KV, T, NT, false> next;
-        next.start(smem, Ks, Vs, begin, a.N - 1, tid);
+        next.start(smem, Ks, Vs, begin, w.low, w.high, tid);
         next.finish(smem, tid);
         __syncthreads();
         // (the two buffers by turns, each with its own code: places in LDS are constants)
         auto step = [&](int u0, auto buf) __attribute__((always_inline)) {
             const unsigned char* kt = smem + decltype(buf)::value * 2 * KV::BYTES;
             unsigned char* to = smem + (decltype(buf)::value ^ 1) * 2 * KV::BYTES;
-            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
+            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, w.low, w.high, tid);
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;
@@ -185,7 +189,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     extern __shared__ __align__(16) unsigned char smem[];    // Q, dO | Q, dO
     __shared__ __align__(16) float stat_z[2][QT], stat_d[2][QT];             // -lse (log2 units), -D
     __shared__ __align__(16) int stat_lo[2][QT];
-    __shared__ int range[NW];
+    __shared__ int2 range[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int skv, tile;
@@ -202,20 +206,33 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
     }
     const float c2 = a.scale * kLog2e;
     // rows that may see a key of the workgroup: from the first key's own on, to the last key's last one
-    const int begin = max(0, k0 - t0) & ~31;
+    int begin = max(0, k0 - t0) & ~31, low = 0, high = a.q - 1;
     const int last = min(k0 + KTILE, a.N) - 1;
     int end = (int)min((int64_t)a.q, (int64_t)last - t0 + a.W);
-    const int2* lo_of = left.lo ? left.lo + (int64_t)(skv * a.G / a.heads) * ((a.q + 31) / 32) : nullptr;
-    if (lo_of) {                                             // ... that belong to the same sequence
-        int most = -1;
-        for (int i = begin / 32 + tid; i < (end + 31) / 32; i += NT)
-            if (lo_of[i].x <= last) most = i;
-        most = wave_max_i(most);
-        if (lane == 0) range[wave] = most;
+    const int4* lo_of = left.lo ? left.lo + (int64_t)(skv * a.G / a.heads) * ((a.q + 31) / 32) : nullptr;
+    if (lo_of) {                                             // ... that belong to the same sequence, and no row of padding at either end
+        low = 0x7fffffff;
+        high = -1;
+        for (int i = begin / 32 + tid; i < (end + 31) / 32; i += NT) {
+            const int4 x = lo_of[i];
+            if (x.x <= last) {
+                low = min(low, x.z);
+                high = max(high, x.w);
+            }
+        }
+        low = wave_min_i(low);
+        high = wave_max_i(high);
+        if (lane == 0) range[wave] = make_int2(low, high);
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < NW; ++w) most = max(most, range[w]);
-        end = min(end, 32 * (__builtin_amdgcn_readfirstlane(most) + 1));
+        for (int w = 0; w < NW; ++w) {
+            low = min(low, range[w].x);
+            high = max(high, range[w].y);
+        }
+        low = __builtin_amdgcn_readfirstlane(low);
+        high = __builtin_amdgcn_readfirstlane(high);
+        begin = max(begin, low & ~31);
+        end = min(end, high + 1);
     }
     f32x16_t ak[MT], av[MT];
 #pragma unroll
@@ -320,9 +337,9 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 #pragma unroll
         for (int x = 0; x < QT / 32; ++x) {
             const int rx = min(r + 32 * x, a.q - 1);
-            lo_next[x] = lo_of ? lo_of[rx / 32] : make_int2(max(0, t0 + rx - a.W + 1), max(0, t0 + rx + 31 - a.W + 1));
+            lo_next[x] = lo_of ? *reinterpret_cast<const int2*>(lo_of + rx / 32) : make_int2(max(0, t0 + rx - a.W + 1), max(0, t0 + rx + 31 - a.W + 1));
         }
-        next.start(smem + buf * 2 * QG::BYTES, Q + base * D, dO + base * D, r, a.q - 1, tid);
+        next.start(smem + buf * 2 * QG::BYTES, Q + base * D, dO + base * D, r, low, high, tid);
     };
     // the tile is there: its rows' statistics go to LDS, too
     auto arrived = [&](int buf) __attribute__((always_inline)) {
@@ -382,7 +399,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_dkdv_kernel(WindowArgs 
 
 // [D of every row][first keys of 32 rows each]
 static size_t rows_bytes(const WindowDims& s) { return a256(sizeof(float) * (size_t)s.bh * s.q); }
-size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int2) * (size_t)s.batch * ((s.q + 31) / 32)); }
+size_t window_backward_ws_bytes(const WindowDims& s) { return rows_bytes(s) + a256(sizeof(int4) * (size_t)s.batch * ((s.q + 31) / 32)); }
 
 template <typename M, int D, int NW, int KT, int QT, int OCCQ, int OCCK, bool DIRECT, int KA, int KB, int QA, int QB>
 static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, const void* V, const void* O,
@@ -394,7 +411,7 @@ static hipError_t backward_t(const WindowDims& s, const void* Q, const void* K, 
     float* Dv = static_cast<float*>(ws);
     const bool few_q = window_few_dq(s), few_k = window_few_dkdv(s);
     if (window_few_both(s)) return launch_window_few_backward(s, Q, K, V, O, lse, dO, first, dQ, dK, dV, Dv, st);
-    int2* lo = first && !few_k ? reinterpret_cast<int2*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr;
+    int4* lo = first && !few_k ? reinterpret_cast<int4*>(static_cast<char*>(ws) + rows_bytes(s)) : nullptr;
     hipError_t e;
     if (few_q) {
         e = launch_window_few_dq(s, Q, K, V, O, lse, dO, first, dQ, Dv, st);

@@ -102,10 +102,11 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
     const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
     const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
+    const int low = a.first ? lo_min : 0, high = a.first ? wave_max_i(lo <= t ? t : -1) : a.N - 1;           // (no other keys are read)
     // the share's keys: a stretch of those that the group's rows can see by their positions
     const int from = max(0, t_min - a.W + 1) / kFewKeys * kFewKeys;
     const int first = max(from + share * each, lo_min == 0x7fffffff ? t_max + 1 : lo_min / kFewKeys * kFewKeys);
-    const int end = min(from + (share + 1) * each, t_max + 1);
+    const int end = min(from + (share + 1) * each, min(t_max, high) + 1);
 
     unsigned char* mine = smem + wave * WAVE_BYTES;
     const float c2 = a.scale * kLog2e;
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             wave_lds_order();
             KV::template store<kWave>(mv, mine, lane);
             wave_lds_order();
-            if (u + NW * kFewKeys < end) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
+            if (u + NW * kFewKeys < end) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, low, high, lane);
         }
         float x[16], top = -INFINITY;
 #pragma unroll
@@ -167,8 +168,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     {
         int u = first + wave * kFewKeys;
         if (u < end) {
-            KV::template load<kWave>(mk, Ks, u, a.N - 1, lane);
-            KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
+            KV::template load<kWave>(mk, Ks, u, low, high, lane);
+            KV::template load<kWave>(mv, Vs, u, low, high, lane);
         }
         for (; u < end; u += NW * kFewKeys) {
             wave_lds_order();                                // (the wave's own LDS: no other wave has to be waited for)
@@ -176,8 +177,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
             if constexpr (!ONE) KV::template store<kWave>(mv, mine + KV::BYTES, lane);
             wave_lds_order();
             if (u + NW * kFewKeys < end) {
-                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
-                if constexpr (!ONE) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
+                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, low, high, lane);
+                if constexpr (!ONE) KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, low, high, lane);
             }
             keys32(u, u + kFewKeys - 1 > t_min, u < lo_max);
         }
@@ -343,6 +344,8 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
     const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
     const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
+    const int low = a.first ? lo_min : 0, high = a.first ? wave_max_i(lo <= t ? t : -1) : a.N - 1;
+    const int u_last = min(t_max, high);
     unsigned char* mine = smem + wave * WAVE_BYTES;
     f32x16_t acc[MT];
 #pragma unroll
@@ -350,18 +353,18 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     {
         u32x4_t mk[KV::template pieces<kWave>], mv[KV::template pieces<kWave>];
         int u = (lo_min == 0x7fffffff ? t_max + 1 : lo_min / kFewKeys * kFewKeys) + wave * kFewKeys;
-        if (u <= t_max) {
-            KV::template load<kWave>(mk, Ks, u, a.N - 1, lane);
-            KV::template load<kWave>(mv, Vs, u, a.N - 1, lane);
+        if (u <= u_last) {
+            KV::template load<kWave>(mk, Ks, u, low, high, lane);
+            KV::template load<kWave>(mv, Vs, u, low, high, lane);
         }
-        for (; u <= t_max; u += NW * kFewKeys) {
+        for (; u <= u_last; u += NW * kFewKeys) {
             wave_lds_order();
             KV::template store<kWave>(mk, mine, lane);
             KV::template store<kWave>(mv, mine + KV::BYTES, lane);
             wave_lds_order();
-            if (u + NW * kFewKeys <= t_max) {
-                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, a.N - 1, lane);
-                KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, a.N - 1, lane);
+            if (u + NW * kFewKeys <= u_last) {
+                KV::template load<kWave>(mk, Ks, u + NW * kFewKeys, low, high, lane);
+                KV::template load<kWave>(mv, Vs, u + NW * kFewKeys, low, high, lane);
             }
             f32x16_t S = f32x16_t{}, dP;
 #pragma unroll
@@ -472,7 +475,7 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
     constexpr int WAVE_BYTES = few_wave_bytes<M, D, false>();
     __shared__ __align__(16) float stat_z[NW][32], stat_d[NW][32];
     __shared__ __align__(16) int stat_lo[NW][32];
-    __shared__ int range[NW];
+    __shared__ int2 range[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int t0 = a.N - a.q, ku = 32 * tile, key = ku + m32;
@@ -484,18 +487,32 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
         load_opnd(v[e], V + own + 16 * e + 8 * h);
     }
     const float c2 = a.scale * kLog2e;
-    const int begin = max(0, ku - t0) & ~31, last = min(ku + 32, a.N) - 1;
+    int begin = max(0, ku - t0) & ~31, low = 0, high = a.q - 1;
+    const int last = min(ku + 32, a.N) - 1;
     int end = (int)min((int64_t)a.q, (int64_t)last - t0 + a.W);
-    if (a.first) {                                           // up to the last row that sees a key
-        int most = -1;
-        for (int r = begin + tid; r < end; r += NW * kWave)
-            if (window_first(a, skv * a.G, r) <= last) most = r;
-        most = wave_max_i(most);
-        if (lane == 0) range[wave] = most;
+    if (a.first) {                                           // from the first to the last row that sees a key; no other is read
+        low = 0x7fffffff;
+        high = -1;
+        for (int r = begin + tid; r < end; r += NW * kWave) {
+            const int lo = window_first(a, skv * a.G, r);
+            if (lo <= min(last, t0 + r)) {
+                low = min(low, r);
+                high = r;
+            }
+        }
+        low = wave_min_i(low);
+        high = wave_max_i(high);
+        if (lane == 0) range[wave] = make_int2(low, high);
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < NW; ++w) most = max(most, range[w]);
-        end = min(end, __builtin_amdgcn_readfirstlane(most) + 1);
+        for (int w = 0; w < NW; ++w) {
+            low = min(low, range[w].x);
+            high = max(high, range[w].y);
+        }
+        low = __builtin_amdgcn_readfirstlane(low);
+        high = __builtin_amdgcn_readfirstlane(high);
+        begin = max(begin, low & ~31);
+        end = min(end, high + 1);
     }
     const int per = begin < end ? (end - begin + 31) / 32 : 0, total = per * a.G;
     unsigned char* mine = smem + wave * WAVE_BYTES;
@@ -512,11 +529,11 @@ __device__ __forceinline__ void few_dkdv(const WindowArgs& a, const T* __restric
         auto fetch = [&](int i) __attribute__((always_inline)) {
             const int s = skv * a.G + i / per, r = begin + i % per * 32;
             const int64_t base = (int64_t)s * a.q;
-            QG::template load<kWave>(mq, Q + base * D, r, a.q - 1, lane);
-            QG::template load<kWave>(mg, dO + base * D, r, a.q - 1, lane);
+            QG::template load<kWave>(mq, Q + base * D, r, low, high, lane);
+            QG::template load<kWave>(mg, dO + base * D, r, low, high, lane);
             const int rr = min(r + m32, a.q - 1);
             nz = -lse[base + rr] * kLog2e;
-            if constexpr (OWN) QG::template load<kWave>(mo, O + base * D, r, a.q - 1, lane);
+            if constexpr (OWN) QG::template load<kWave>(mo, O + base * D, r, low, high, lane);
             else nd = -Dv[base + rr];
             nl = window_first(a, s, rr);
         };

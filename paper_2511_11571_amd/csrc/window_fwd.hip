@@ -30,7 +30,7 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     constexpr int NT = NW * kWave, QT = 32 * NW, STEPS = D / 16, MT = D / 32;
     using KV = Tile<M, D, KT>;
     extern __shared__ __align__(16) unsigned char smem[];    // K, V | K, V
-    __shared__ int wg_lo[NW];
+    __shared__ int2 wg_keys[NW];
     const int tid = threadIdx.x, lane = tid % kWave, h = lane >> 5, m32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int skv, pos;
@@ -44,8 +44,8 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     Opnd<M> q[STEPS];
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) load_opnd(q[e], Q + row * D + 16 * e + 8 * h);
-    const WaveKeys k = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_lo);
-    const int begin = k.begin, end = t0 + min((tile + 1) * QT, a.q);         // (begin beyond it: nobody attends anything)
+    const WaveKeys k = wave_keys<NW>(a, t0, tile * QT, r0, t, lo, wave, lane, wg_keys);
+    const int begin = k.begin, end = min(t0 + min((tile + 1) * QT, a.q), k.high + 1);        // (begin beyond it: nobody attends anything)
 
     const float c2 = a.scale * kLog2e;
     f32x16_t acc[MT];
@@ -96,14 +96,14 @@ __global__ __launch_bounds__(NW* kWave, OCC) void window_forward_kernel(WindowAr
     };
     if (begin < end) {
         Coming<KV, T, NT, false> next;
-        next.start(smem, Ks, Vs, begin, a.N - 1, tid);
+        next.start(smem, Ks, Vs, begin, k.low, k.high, tid);
         next.finish(smem, tid);
         __syncthreads();
         // (the two buffers by turns, each with its own code: places in LDS are constants)
         auto step = [&](int u0, auto buf) __attribute__((always_inline)) {
             const unsigned char* kt = smem + decltype(buf)::value * 2 * KV::BYTES;
             unsigned char* to = smem + (decltype(buf)::value ^ 1) * 2 * KV::BYTES;
-            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, a.N - 1, tid);
+            if (u0 + KT < end) next.start(to, Ks, Vs, u0 + KT, k.low, k.high, tid);
 #pragma unroll
             for (int x = 0; x < KT / 32; ++x) {
                 const int u = u0 + 32 * x;

@@ -124,13 +124,13 @@ struct Tile {
     // what NT threads move from memory to LDS: `pieces` of every thread
     template <int NT>
     static constexpr int pieces = ROWS * PIECES / NT;
-    // rows first .. first + ROWS of a slice, rows from last + 1 on replaced by row `last`
+    // rows first .. first + ROWS of a slice, those outside low .. high replaced by the nearer of the two
     template <int NT>
-    static __device__ __forceinline__ void load(u32x4_t (&x)[ROWS * PIECES / NT], const T* __restrict__ slice, int first, int last, int tid)
+    static __device__ __forceinline__ void load(u32x4_t (&x)[ROWS * PIECES / NT], const T* __restrict__ slice, int first, int low, int high, int tid)
     {
         static_assert(ROWS * PIECES % NT == 0 && (NT % PIECES == 0), "whole pieces");
         constexpr int STEP = NT / PIECES;
-        if (first + ROWS - 1 <= last) {                      // (one offset for all lanes' pieces, the rest is scalar)
+        if (first >= low && first + ROWS - 1 <= high) {                      // (one offset for all lanes' pieces, the rest is scalar)
             const char* from = reinterpret_cast<const char*>(slice) + (int64_t)first * RB;
             const uint32_t at = 16u * (uint32_t)tid;
 #pragma unroll
@@ -139,7 +139,7 @@ struct Tile {
             const int row = first + tid / PIECES;
 #pragma unroll
             for (int i = 0; i < ROWS * PIECES / NT; ++i)
-                x[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(slice) + (int64_t)min(row + i * STEP, last) * RB + 16 * (tid % PIECES));
+                x[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(slice) + (int64_t)min(max(row + i * STEP, low), high) * RB + 16 * (tid % PIECES));
         }
     }
     template <int NT>
@@ -155,14 +155,14 @@ struct Tile {
     // The same straight into LDS: a wave's instruction fills 1 KB, so a lane fetches the piece that belongs at its place.
     // The caller waits (fetched()) before the barrier after which the tile is read.
     template <int NT>
-    static __device__ __forceinline__ void fetch(unsigned char* tile, const T* __restrict__ slice, int first, int last, int tid)
+    static __device__ __forceinline__ void fetch(unsigned char* tile, const T* __restrict__ slice, int first, int low, int high, int tid)
     {
         static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0, "whole pieces");
         const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
 #pragma unroll
         for (int i = 0; i < ROWS * PIECES / NT; ++i) {
             const int row = tid / PIECES + i * (NT / PIECES);
-            const char* at = reinterpret_cast<const char*>(slice) + (int64_t)min(first + row, last) * RB + 16 * ((tid % PIECES) ^ place(row));
+            const char* at = reinterpret_cast<const char*>(slice) + (int64_t)min(max(first + row, low), high) * RB + 16 * ((tid % PIECES) ^ place(row));
             const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile + 16 * (i * NT + wave * kWave));
             // (by hand: the compiler would wait for the builtin's loads before the next read of any LDS)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(at) : "memory", "m0");
@@ -212,12 +212,12 @@ struct Tile<Split, D, ROWS> {
     template <int NT>
     static constexpr int pieces = 2 * ROWS * PIECES / NT;    // (eight fp32 elements make a piece of each part)
     template <int NT>
-    static __device__ __forceinline__ void load(u32x4_t (&x)[2 * ROWS * PIECES / NT], const float* __restrict__ slice, int first, int last, int tid)
+    static __device__ __forceinline__ void load(u32x4_t (&x)[2 * ROWS * PIECES / NT], const float* __restrict__ slice, int first, int low, int high, int tid)
     {
         static_assert(ROWS * PIECES % NT == 0 && NT % PIECES == 0, "whole pieces");
 #pragma unroll
         for (int i = 0; i < ROWS * PIECES / NT; ++i) {
-            const int row = min(first + tid / PIECES + i * (NT / PIECES), last);
+            const int row = min(max(first + tid / PIECES + i * (NT / PIECES), low), high);
             const u32x4_t* p = reinterpret_cast<const u32x4_t*>(slice + (int64_t)row * D + 8 * (tid % PIECES));
             x[2 * i] = p[0];
             x[2 * i + 1] = p[1];
@@ -277,14 +277,14 @@ template <class TILE, typename T, int NT, bool DIRECT>
 struct Coming {
     static constexpr int P = DIRECT ? 1 : TILE::template pieces<NT>;
     u32x4_t x[P], y[P];
-    __device__ __forceinline__ void start(unsigned char* to, const T* __restrict__ a, const T* __restrict__ b, int first, int last, int tid)
+    __device__ __forceinline__ void start(unsigned char* to, const T* __restrict__ a, const T* __restrict__ b, int first, int low, int high, int tid)
     {
         if constexpr (DIRECT) {
-            TILE::template fetch<NT>(to, a, first, last, tid);
-            TILE::template fetch<NT>(to + TILE::BYTES, b, first, last, tid);
+            TILE::template fetch<NT>(to, a, first, low, high, tid);
+            TILE::template fetch<NT>(to + TILE::BYTES, b, first, low, high, tid);
         } else {
-            TILE::template load<NT>(x, a, first, last, tid);
-            TILE::template load<NT>(y, b, first, last, tid);
+            TILE::template load<NT>(x, a, first, low, high, tid);
+            TILE::template load<NT>(y, b, first, low, high, tid);
         }
     }
     // (a barrier has to follow)
@@ -323,12 +323,14 @@ __device__ __forceinline__ int wave_min_i(int x)
 __device__ __forceinline__ int wave_max_i(int x) { return -wave_min_i(-x); }
 
 // Keys that a wave's 32 rows from r0 on attend: some of them those from lo_min to t_max, all of them those from lo_max to
-// t_min; begin: a multiple of 32 that is not behind the first key of the workgroup, whose rows start at wg_r0.
+// t_min.  begin: a multiple of 32 that is not behind the first key of the workgroup, whose rows start at wg_r0.  With first keys
+// low .. high hold all that some row of the workgroup attends, and no other row is read: padding may hold anything.
+// live_min, live_max: positions of the wave's first and last row that attend something.
 struct WaveKeys {
-    int lo_min, lo_max, t_min, t_max, begin;
+    int lo_min, lo_max, t_min, t_max, begin, low, high, live_min, live_max;
 };
 template <int NW>
-__device__ __forceinline__ WaveKeys wave_keys(const WindowArgs& a, int t0, int wg_r0, int r0, int t, int lo, int wave, int lane, int* wg_lo)
+__device__ __forceinline__ WaveKeys wave_keys(const WindowArgs& a, int t0, int wg_r0, int r0, int t, int lo, int wave, int lane, int2* wg_keys)
 {
     WaveKeys k;
     k.t_min = t0 + min(r0, a.q - 1);
@@ -337,16 +339,26 @@ __device__ __forceinline__ WaveKeys wave_keys(const WindowArgs& a, int t0, int w
         k.lo_min = r0 < a.q ? max(0, k.t_min - a.W + 1) : 0x7fffffff;
         k.lo_max = max(0, k.t_max - a.W + 1);
         k.begin = max(0, t0 + wg_r0 - a.W + 1) & ~31;
+        k.low = 0;
+        k.high = a.N - 1;
         return k;
     }
-    k.lo_min = r0 < a.q ? wave_min_i(lo <= t ? lo : 0x7fffffff) : 0x7fffffff;
+    const bool live = r0 < a.q && lo <= t;
+    k.lo_min = wave_min_i(live ? lo : 0x7fffffff);
     k.lo_max = wave_max_i(lo);
-    if (lane == 0) wg_lo[wave] = k.lo_min;
+    k.live_min = wave_min_i(live ? t : 0x7fffffff);
+    k.live_max = wave_max_i(live ? t : -1);
+    if (lane == 0) wg_keys[wave] = make_int2(k.lo_min, k.live_max);
     __syncthreads();
-    int begin = wg_lo[0];
+    int low = wg_keys[0].x, high = wg_keys[0].y;
 #pragma unroll
-    for (int w = 1; w < NW; ++w) begin = min(begin, wg_lo[w]);
-    k.begin = __builtin_amdgcn_readfirstlane(begin) & ~31;
+    for (int w = 1; w < NW; ++w) {
+        low = min(low, wg_keys[w].x);
+        high = max(high, wg_keys[w].y);
+    }
+    k.low = __builtin_amdgcn_readfirstlane(low);
+    k.high = __builtin_amdgcn_readfirstlane(high);
+    k.begin = k.low & ~31;
     return k;
 }
 
