@@ -313,12 +313,16 @@ int moba_decode_forward_ws(const moba_shape* shape, int32_t q_len, const void* Q
 typedef struct moba_window_shape {
     int32_t batch, heads;
     int32_t kv_heads;      /* grouped-query / multi-query attention, as in moba_shape; 0 = heads   */
-    int32_t q_len, kv_len; /* the queries are the LAST q_len of kv_len positions (training: equal) */
+    int32_t q_len, kv_len; /* the queries are the LAST q_len of kv_len positions (training: equal), in every
+                            * batch entry: caches of unequal lengths are held at the END of their rows, with
+                            * first_key as their first row                                       */
     int32_t kv_rows;       /* rows that a slice of K and V (and dK, dV) takes in memory, e.g. a cache
                             * with room to grow; 0 = kv_len.  Rows from kv_len on are neither read
                             * nor written.                                                       */
     int32_t head_dim;      /* 64 or 128                                                          */
-    int32_t window;        /* keys that a query attends, itself included; 0 = all up to itself   */
+    int32_t window;        /* keys that a query attends, itself included; 0 = all up to itself.  Packed
+                            * batches of a dense layer: the longest sequence's length gives the same results and
+                            * lets the choice of kernels and the sharing of keys go by it             */
     int32_t dtype;         /* moba_dtype                                                         */
     float   softmax_scale; /* <= 0 selects 1/sqrt(head_dim)                                      */
 } moba_window_shape;

@@ -19,7 +19,9 @@
 // 0.78 | 1.15 ms (1030 | 930); 16 of 32768, d = 64, W = 256 102 | 150 us.  Slower for dK and dV at d = 64: three waves a SIMD by tiles of 32
 // queries 640, of 64 (10 registers spilled) 680; two or eight waves to a workgroup 655 and 605, at W = 256 158 and 200.
 // Operands are asked for one product ahead of their use where registers allow, which gains 1 to 2 %, for dQ at d = 128 5 %; two or three ahead
-// the same, or as many registers spilled as to cost 15 to 60 %.
+// the same, or as many registers spilled as to cost 15 to 60 %.  Spilled as it is: dQ at d = 64 and dK and dV at d = 128 five registers each, fp32
+// dK and dV at d = 64 one.  fp32 at d = 128: three parts of a wave's own Q and dO, or K and V, are 192 registers, and dQ takes 414, dK and
+// dV 437 of them in all, which leaves one wave a SIMD: 16 heads of 8192, W = 256 0.54 ms, 2.8 times what its products take.
 #include "window_tiles.h"
 
 namespace moba {

@@ -8,8 +8,13 @@
 // kernel merges their parts, in their order.  The backward's waves share the walk of dQ's rows, and of dK's and dV's keys, alike.
 //
 // What bounds it: with many keys, how fast they come in -- 4 positions of 16 heads on 4 against 131109 keys, d = 128 50 us, 5.4 TB/s (a copy of
-// that size runs at 5.4), 6 of them the second kernel; with few, the chain of steps: a position against 256 keys 4.4 us, fp32, 2
-// heads of 2048, W = 256 12 us forward and 22 backward.
+// that size runs at 5.4), 6 of them the second kernel, fp32 107 us, 5.0 TB/s; with few, the chain of steps: a position against 256 keys 4.5 us,
+// fp32, 2 heads of 2048, W = 256 11 us forward and 20 backward.
+//
+// Roundings are those of the tiled kernels: bf16 P and dS enter their products in bf16, half a step of 2^-9 each, after the sums of P and
+// with D in fp32; everything else is fp32.  A token's O is 1.9e-3 off 64 bits in the 2-norm where its own rounding is 1.7e-3.
+//
+// fp32 at d = 128, backward, takes fp32 products and more registers than there are: both directions in one launch spill 88, dK and dV alone 25.
 #include <algorithm>
 
 #include "window_tiles.h"
@@ -728,6 +733,10 @@ static int few_shares(const WindowDims& s)
 // 236 | 194; 8192 567 | 668; d = 128, W = 256: N = 1024 46.1 | 42.5; 2048 50.1 | 80.1; dense 2048 176 | 162, 4096 412 | 502.
 // fp32, dense: d = 64 forward 4096 294 | 301, on 4 heads 240 | 303; 2048 106 | 86; 4 heads of 8192 400 | 293; d = 128 2048 189 | 170, 4096 421 | 604;
 // backward 2048 562 | 633, 1024 293 | 188.
+// The last positions of a longer sequence, forward, dense, bf16: against 131072 keys, 16 heads on 4, d = 128: 64 2760 | 153, 1024 2872 | 1729, 2048
+// 3052 | 3278, 4096 4616 | 6373; 16 heads, d = 64: 1024 2390 | 1020, 2048 2416 | 1878, 4096 3049 | 3547; 4 heads: 4096 2342 | 990.  Against 32768, 16 on 4,
+// d = 128: 1024 745 | 440, 2048 750 | 789; 16, d = 64: 2048 571 | 451, 4096 678 | 816.  The rule takes the faster one of each pair.  First keys it does not
+// know: a packed batch counts as one sequence, of its window's length where that is given.
 static bool few_tiles(const WindowDims& s, double tiles, double walk, double longest, double c)
 {
     return tiles * walk < c * longest - (s.D == 64 ? 24000 : 12000);

@@ -15,9 +15,10 @@
 // heads on 4 of 16384, d = 128, dense 1.13 ms, 970 TFLOP/s (a library product of 8192^3 1330); 32 of 8192, d = 64, dense 0.38 ms, 725;
 // W = 256, 16 of 32768, d = 64 78 us: 3.4 TB/s of Q, K, V and O, a wave has 9 lots and as much again to begin and end.
 // Slower, us at W = 256, 16 heads of 8192 (25 as it is): 64 queries to a wave 31, two waves to a workgroup 35, eight 26, tiles
-// of 32 keys 26, two lots at once 29, tiles straight into LDS 26; priorities for the products, dense 16384: 1.11 -> 1.21 ms;
-// without operands read ahead of their products 1 to 2 % at each size; weights by the old reference first and a maximum only
-// where they come out large, at three waves a SIMD (four spill): 16 of 32768, W = 256 76 -> 83, 32 of 8192, dense 371 -> 352.
+// of 32 keys 26, two lots at once 29; priorities for the products, dense 16384: 1.11 -> 1.21 ms; without operands read
+// ahead of their products 1 to 2 % at each size.  Slower there and faster for long walks: weights by the old reference first and a
+// maximum only where they come out large, at three waves a SIMD (four spill): 16 of 32768, W = 256 76 -> 83, 32 of 8192, dense 371 ->
+// 352; tiles straight into LDS, 23 -> 24 and 379 -> 358.
 #include "window_tiles.h"
 
 namespace moba {

@@ -270,9 +270,10 @@ __device__ __forceinline__ void wave_lds_order()
 __device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Two tiles, one behind the other in LDS, on their way while a workgroup of NT threads works on two others: through
-// registers, or (DIRECT) straight into LDS, which takes fewer registers but costs time where there are enough: d = 64,
-// 2 x 16 heads of 8192, dense, us through registers -> direct: dQ 424 -> 451, dK and dV 603 -> 648; d = 128, 16 heads
-// on 4 of 32768, W = 2048: forward 622 -> 636, dQ 845 -> 880, dK and dV 1793 -> 1305 (24 registers spilled -> 10).
+// registers, or (DIRECT) straight into LDS, which takes fewer registers.  us through registers | direct, d = 64: forward, 16 heads of
+// 8192, W = 256 22.9 | 24.1, 2 x 16 of 8192, dense 379 | 358, both backward kernels 1045 | 1031 (dQ direct), 1042 | 1035 (dK and dV); d = 128, 16
+// heads on 4 of 32768, W = 2048: forward 592 | 573, backward 1969 | 1953 (dQ), 2485 | 1930 (dK and dV; 26 registers spilled | 5).  Taken
+// where it saves spilled registers, in dK and dV at d = 128; the forward keeps to the side of short windows.
 template <class TILE, typename T, int NT, bool DIRECT>
 struct Coming {
     static constexpr int P = DIRECT ? 1 : TILE::template pieces<NT>;
