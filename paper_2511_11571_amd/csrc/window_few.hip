@@ -12,7 +12,9 @@
 // fp32, 2 heads of 2048, W = 256 11 us forward and 20 backward.
 //
 // Roundings are those of the tiled kernels: bf16 P and dS enter their products in bf16, half a step of 2^-9 each, after the sums of P and
-// with D in fp32; everything else is fp32.  A token's O is 1.9e-3 off 64 bits in the 2-norm where its own rounding is 1.7e-3.
+// with D in fp32; everything else is fp32.  A token's O is 2.0e-3 off 64 bits in the 2-norm where its own rounding is 1.7e-3; P in two parts
+// would take that off for 2 to 6 % of a token's time (5.3 -> 5.6 us against 256 keys, 20.1 -> 21.1 for 16 positions of 16 heads on 4
+// against 32768) and 6 to 20 % of a short prompt's (16 of 2048, dense 21.4 -> 24.7).
 //
 // fp32 at d = 128, backward, takes fp32 products and more registers than there are: both directions in one launch spill 88, dK and dV alone 25.
 #include <algorithm>
@@ -41,6 +43,13 @@ constexpr int few_wave_bytes()
 // parts of rows shared by workgroups: [slice][32 rows each][share][row][m (log2 units), l, O]
 template <int D>
 constexpr int kPartWords = D + 2;
+
+// position of the last of a wave's rows, in order in its lanes 0 .. 31 and again 32 .. 63, that attends something; -1: of none
+__device__ __forceinline__ int last_live(int lo, int t)
+{
+    const uint32_t live = (uint32_t)__ballot(lo <= t);
+    return live ? __builtin_amdgcn_readlane(t, 31 - __builtin_clz(live)) : -1;
+}
 
 // O of 32 rows of every wave through LDS, 16-byte pieces of row m exchanged by m & 7; then every thread takes CH
 // channels ch0 .. of row c
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, sizeof(T) == 2 ? 2 : 1) void wind
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
     const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
     const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
-    const int low = a.first ? lo_min : 0, high = a.first ? wave_max_i(lo <= t ? t : -1) : a.N - 1;           // (no other keys are read)
+    const int low = a.first ? lo_min : 0, high = a.first ? last_live(lo, t) : a.N - 1;           // (no other keys are read)
     // the share's keys: a stretch of those that the group's rows can see by their positions
     const int from = max(0, t_min - a.W + 1) / kFewKeys * kFewKeys;
     const int first = max(from + share * each, lo_min == 0x7fffffff ? t_max + 1 : lo_min / kFewKeys * kFewKeys);
@@ -349,7 +358,7 @@ __device__ __forceinline__ void few_dq(const WindowArgs& a, const T* __restrict_
     const int t_min = t0 + 32 * group / a.G, t_max = t0 + min(32 * group + 31, rows - 1) / a.G;
     const int lo_min = a.first ? wave_min_i(lo <= t ? lo : 0x7fffffff) : max(0, t_min - a.W + 1);
     const int lo_max = a.first ? wave_max_i(lo) : max(0, t_max - a.W + 1);
-    const int low = a.first ? lo_min : 0, high = a.first ? wave_max_i(lo <= t ? t : -1) : a.N - 1;
+    const int low = a.first ? lo_min : 0, high = a.first ? last_live(lo, t) : a.N - 1;
     const int u_last = min(t_max, high);
     unsigned char* mine = smem + wave * WAVE_BYTES;
     f32x16_t acc[MT];

@@ -344,11 +344,12 @@ __device__ __forceinline__ WaveKeys wave_keys(const WindowArgs& a, int t0, int w
         k.high = a.N - 1;
         return k;
     }
-    const bool live = r0 < a.q && lo <= t;
-    k.lo_min = wave_min_i(live ? lo : 0x7fffffff);
+    const bool mine = r0 + (lane & 31) < a.q && lo <= t;
+    const uint32_t live = (uint32_t)__ballot(mine);          // (lanes 32 .. 63 hold the same rows)
+    k.lo_min = wave_min_i(mine ? lo : 0x7fffffff);
     k.lo_max = wave_max_i(lo);
-    k.live_min = wave_min_i(live ? t : 0x7fffffff);
-    k.live_max = wave_max_i(live ? t : -1);
+    k.live_min = live ? t0 + r0 + __builtin_ctz(live) : 0x7fffffff;
+    k.live_max = live ? t0 + r0 + 31 - __builtin_clz(live) : -1;
     if (lane == 0) wg_keys[wave] = make_int2(k.lo_min, k.live_max);
     __syncthreads();
     int low = wg_keys[0].x, high = wg_keys[0].y;
